@@ -1,0 +1,96 @@
+/*
+ * dropit_layers.h -- C ABI of the operators that stand beside the dropped cache in a training step:
+ *
+ *   the gated projection of a feed-forward block and its backward pass   -> dropit_gated_forward, dropit_gated_backward
+ *   the AdamW step over many tensors, states in 32 or in 8 bits          -> dropit_adamw, dropit_adamw_unpack
+ *   the global gradient norm and the factor that clips it                -> dropit_grad_norm
+ *
+ * The conventions of dropit.h hold: device pointers owned by the caller, nothing allocated or kept, all work
+ * enqueued on `hip_stream`, no host synchronisation, arguments validated before any HIP call, status codes
+ * instead of aborts, results bit-reproducible run to run, distinct workspaces for concurrent calls.  Every call
+ * uses ordinary kernel launches only and can be captured into a HIP graph.
+ */
+#ifndef DROPIT_LAYERS_H
+#define DROPIT_LAYERS_H
+
+#include "dropit.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/*
+ * AdamW over many tensors at once.  For every element, with t the step (1 for the first) and s the value at
+ * `grad_scale` (1 if NULL), in fp32, each operation rounded by itself (no fused multiply-adds):
+ *     g = s * grad
+ *     m = beta1 * m + (1 - beta1) * g
+ *     v = beta2 * v + (1 - beta2) * (g * g)
+ *     p = p * (1 - lr * weight_decay) - m / (sqrt(v) * (1 / sqrt(1 - beta2^t)) + eps) * (lr / (1 - beta1^t))
+ * The scalars are evaluated in double and rounded once.
+ *
+ * Parameters: fp32; bf16 (rounded to nearest even); or bf16 with a residual, 16 more bits that make it an exact
+ * fp32 master: pattern(master) = (pattern(p) << 16) + residual (a signed sum), p being master rounded to nearest,
+ * ties away from zero.  A residual of zeros starts from the bf16 values as they are.
+ *
+ * States of 32 bits are fp32.  States of 8 bits are codes in blocks of DROPIT_ADAMW_BLOCK consecutive elements
+ * of a tensor that share an int16 offset: with b the fp32 pattern of |value| and B the block's largest,
+ *     offset = max(min((B + 0xfffff) >> 20, 0x7f7) - top, 0)          top = 127 for m, 255 for v
+ *     code   = clamp(min((b + d) >> 20, 0x7f7) - offset, 0, top)      m: plus 128 where the value is negative
+ * and a code c > 0 (its low seven bits for m) stands for the fp32 pattern (c + offset) << 20, 0 for zero: three
+ * bits of mantissa, 15.9 octaves below the block's largest for m, 31.75 for v.  A v below that takes code 1, not
+ * 0, unless it is zero, so a small v never turns into a division by eps.  d is a dither in [0, 2^20): the upper 20
+ * bits of i * 0x6a09e667 + t * 0x9e3779b9 (mod 2^32) for element i of its tensor, complemented for v.  Over the
+ * steps it takes every value equally often, so the rounding is right on average; rounding to nearest would hold
+ * an average of 1 - beta2 = 0.001 where it is.  A block with an infinity or a NaN decodes to NaN throughout.
+ * Codes and offsets of zeros are states of zeros.
+ */
+#define DROPIT_ADAMW_BLOCK 256
+typedef struct {
+    void *p;                   /* numel parameters, updated */
+    const void *g;             /* numel gradients */
+    void *m, *v;               /* numel states each, fp32 or 8-bit codes, updated */
+    int16_t *m_offset;         /* 8-bit states: ceil(numel / DROPIT_ADAMW_BLOCK) offsets each, updated; else NULL */
+    int16_t *v_offset;
+    int16_t *residual;         /* numel residuals of bf16 parameters, updated, or NULL; NULL for all tensors of a call or none */
+    int64_t numel;             /* 0 .. 2^34 */
+} dropit_adamw_tensor;
+
+typedef struct {
+    double lr, beta1, beta2, eps, weight_decay;   /* finite; betas in [0, 1), eps >= 0 */
+    int64_t step;                                 /* t >= 1, unless step_device is given */
+    const int32_t *step_device;                   /* device, or NULL: t is read there when the kernels run (>= 1), so that a
+                                                     captured graph can be replayed with another t */
+    const float *grad_scale;                      /* device, or NULL */
+} dropit_adamw_hyper;
+
+/*
+ * tensors    host array of `count` entries (count >= 0), read during the call only.  Pointers need the alignment of
+ *            their element type; where all of a tensor's are 16-byte aligned (8 for codes) it moves in wide accesses.
+ *            A tensor's storage appears once in a call.
+ * p_dtype, g_dtype  of all tensors; state_bits 32 or 8
+ */
+dropit_status dropit_adamw(const dropit_adamw_tensor *tensors, int64_t count, dropit_dtype p_dtype, dropit_dtype g_dtype,
+                           int state_bits, const dropit_adamw_hyper *hyper, void *hip_stream);
+
+/* The values that 8-bit states stand for, as bf16 (which holds them exactly): codes [numel], offsets
+ * [ceil(numel / DROPIT_ADAMW_BLOCK)], is_signed 1 for m and 0 for v, values [numel] out; numel 0 .. 2^34. */
+dropit_status dropit_adamw_unpack(const uint8_t *codes, const int16_t *offsets, int64_t numel, int is_signed,
+                                  void *values, void *hip_stream);
+
+/*
+ * The 2-norm over all elements of `count` tensors, and the factor that brings it to at most max_norm:
+ *     out[0] = sqrt(sum of squares),  out[1] = min(1, max_norm / (out[0] + 1e-6))         (device fp32)
+ * Squares and a thread's sum of 64 of them in fp32, everything above in fp64, in a fixed order.  A NaN norm gives a
+ * NaN factor, an infinite one the factor 0.  max_norm > 0, infinity for a factor of 1.
+ * grads [count] device pointers with the alignment of their type, numels [count] 0 .. 2^34, dtypes [count] dropit_dtype: host
+ * arrays.  workspace: device, 256-byte aligned, >= dropit_grad_norm_workspace_bytes of the same numels and count
+ * (0 on invalid arguments or where none is needed).
+ */
+size_t dropit_grad_norm_workspace_bytes(const int64_t *numels, int64_t count);
+dropit_status dropit_grad_norm(const void *const *grads, const int64_t *numels, const int32_t *dtypes, int64_t count,
+                               double max_norm, float *out, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* DROPIT_LAYERS_H */

@@ -28,3 +28,8 @@ from .binding import (  # noqa: F401
     weight_grad_workspace_bytes,
     weight_grad_path,
 )
+from .layers import (  # noqa: F401
+    adamw,
+    adamw_unpack,
+    grad_norm,
+)

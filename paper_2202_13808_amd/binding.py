@@ -97,6 +97,15 @@ def lib() -> ctypes.CDLL:
         L.dropit_trace_events.argtypes = [ctypes.POINTER(vp), i32]
         L.dropit_weight_grad.restype = i32
         L.dropit_weight_grad.argtypes = [vp, vp, i64, p64, i32, i32, vp, i64, pconv, vp, vp, sz, vp]
+        # dropit_layers.h (marshalled in layers.py)
+        L.dropit_adamw.restype = i32
+        L.dropit_adamw.argtypes = [vp, i64, i32, i32, i32, vp, vp]
+        L.dropit_adamw_unpack.restype = i32
+        L.dropit_adamw_unpack.argtypes = [vp, vp, i64, i32, vp, vp]
+        L.dropit_grad_norm_workspace_bytes.restype = sz
+        L.dropit_grad_norm_workspace_bytes.argtypes = [vp, i64]
+        L.dropit_grad_norm.restype = i32
+        L.dropit_grad_norm.argtypes = [vp, vp, vp, i64, dbl, vp, vp, sz, vp]
         _lib = L
     return _lib
 

@@ -1,0 +1,235 @@
+// The global 2-norm of many tensors and the factor that clips it (dropit_layers.h).
+//
+// Bound by reading the gradients once.  A workgroup sums a chunk of 16 K elements and writes one fp64 partial; a single
+// workgroup then adds the partials in ascending order of thread and slot, so the result does not depend on who finished
+// first.  The pointers travel in the kernel's arguments, as in adamw.hip.  A few chunks (a few biases, a tiny model): one workgroup does it all: the second launch would cost more than the first saves.
+#include <cmath>
+
+#include "common.hpp"
+#include "dropit_layers.h"
+
+namespace dropit {
+namespace {
+
+constexpr int NORM_THREADS = 256;
+constexpr int NORM_PER_THREAD = 64;
+constexpr int NORM_CHUNK = NORM_THREADS * NORM_PER_THREAD;
+constexpr int NORM_TENSORS = 160;                      // 160 x 24 bytes: arguments stay under 4 KB
+constexpr int64_t NORM_MAX_NUMEL = int64_t(1) << 34;
+constexpr int FINAL_THREADS = 1024;
+constexpr uint32_t NORM_MAX_CHUNKS = 1u << 23;         // of a launch: fewer than 2^32 threads
+
+struct NormTable {
+    const void *g[NORM_TENSORS];
+    int64_t numel_bf16[NORM_TENSORS];                  // numel * 2 + (1 if bf16)
+    uint32_t first[NORM_TENSORS];
+    int count;
+};
+static_assert(sizeof(NormTable) + 16 <= 4096, "kernel arguments");
+
+typedef __attribute__((ext_vector_type(4))) uint32_t nu32x4;
+
+// the sum of `v` over the workgroup, in thread 0, in a fixed order
+template <int THREADS>
+__device__ inline double workgroup_sum(double v, double *part)
+{
+#pragma unroll
+    for (int o = WAVE / 2; o > 0; o >>= 1) v += __shfl_xor(v, o, WAVE);
+    __syncthreads();
+    if ((threadIdx.x & (WAVE - 1)) == 0) part[threadIdx.x / WAVE] = v;
+    __syncthreads();
+    double s = 0.0;
+    if (threadIdx.x == 0)
+        for (int w = 0; w < THREADS / WAVE; ++w) s += part[w];
+    return s;
+}
+
+__device__ inline void add_square(float &acc, float x) { acc = fmaf(x, x, acc); }
+
+__device__ inline void add_squares(float (&acc)[4], nu32x4 w, bool bf16)
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        if (bf16) {
+            add_square(acc[e], __uint_as_float(w[e] << 16));
+            add_square(acc[e], __uint_as_float(w[e] & 0xffff0000u));
+        } else {
+            add_square(acc[e], __uint_as_float(w[e]));
+        }
+    }
+}
+
+// this thread's share of the squares of a chunk: at most 64 elements, in four fp32 sums
+__device__ inline double chunk_squares(const void *g, int64_t numel, bool bf16, int64_t chunk0)
+{
+    float acc[4] = {0.f, 0.f, 0.f, 0.f};
+    const int tid = threadIdx.x;
+    const int n = int(min<int64_t>(numel - chunk0, NORM_CHUNK));
+    const char *base = static_cast<const char *>(g) + chunk0 * (bf16 ? 2 : 4);
+    if ((reinterpret_cast<uintptr_t>(base) & 15u) == 0) {
+        // 16-byte loads, eight of them (16 of fp32) in flight, then the elements behind the last whole one
+        const int per = bf16 ? 8 : 4, vecs = n / per;
+        for (int r0 = 0; r0 < vecs; r0 += 8 * NORM_THREADS) {
+            nu32x4 w[8];
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+                const int at = r0 + r * NORM_THREADS + tid;
+                w[r] = at < vecs ? reinterpret_cast<const nu32x4 *>(base)[at] : nu32x4{0u, 0u, 0u, 0u};
+            }
+#pragma unroll
+            for (int r = 0; r < 8; ++r) add_squares(acc, w[r], bf16);
+        }
+        const int at = vecs * per + tid;
+        if (at < n)
+            add_square(acc[0], bf16 ? __uint_as_float(uint32_t(reinterpret_cast<const uint16_t *>(base)[at]) << 16)
+                                    : reinterpret_cast<const float *>(base)[at]);
+    } else {
+        for (int i0 = tid; i0 < n; i0 += 8 * NORM_THREADS) {
+            float x[8];
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+                const int at = i0 + r * NORM_THREADS;
+                x[r] = 0.f;
+                if (at < n) x[r] = bf16 ? __uint_as_float(uint32_t(reinterpret_cast<const uint16_t *>(base)[at]) << 16)
+                                        : reinterpret_cast<const float *>(base)[at];
+            }
+#pragma unroll
+            for (int r = 0; r < 8; ++r) add_square(acc[r & 3], x[r]);
+        }
+    }
+    return (double(acc[0]) + double(acc[1])) + (double(acc[2]) + double(acc[3]));
+}
+
+__device__ inline void write_norm(double sum, double max_norm, float *out)
+{
+    const float norm = float(sqrt(sum));
+    const float factor = float(max_norm) / (norm + 1e-6f);
+    out[0] = norm;
+    out[1] = max_norm > 3.4028234663852886e38 ? 1.f : factor > 1.f ? 1.f : factor;       // (a NaN stays one)
+}
+
+__global__ void __launch_bounds__(NORM_THREADS)
+norm_chunks_kernel(const NormTable table, double *__restrict__ partial)
+{
+    __shared__ double part[NORM_THREADS / WAVE];
+    int lo = 0, hi = table.count - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (table.first[mid] <= blockIdx.x) lo = mid; else hi = mid - 1;
+    }
+    const int64_t nb = table.numel_bf16[lo];
+    const double s = workgroup_sum<NORM_THREADS>(
+        chunk_squares(table.g[lo], nb >> 1, nb & 1, int64_t(blockIdx.x - table.first[lo]) * NORM_CHUNK), part);
+    if (threadIdx.x == 0) partial[blockIdx.x] = s;
+}
+
+__global__ void __launch_bounds__(NORM_THREADS)
+norm_small_kernel(const NormTable table, uint32_t chunks, double max_norm, float *__restrict__ out)
+{
+    __shared__ double part[NORM_THREADS / WAVE];
+    double v = 0.0;
+    for (int t = 0; t < table.count; ++t) {
+        const int64_t nb = table.numel_bf16[t];
+        const uint32_t end = t + 1 < table.count ? table.first[t + 1] : chunks;
+        for (uint32_t c = 0; c < end - table.first[t]; ++c) v += chunk_squares(table.g[t], nb >> 1, nb & 1, int64_t(c) * NORM_CHUNK);
+    }
+    const double s = workgroup_sum<NORM_THREADS>(v, part);
+    if (threadIdx.x == 0) write_norm(s, max_norm, out);
+}
+
+__global__ void __launch_bounds__(FINAL_THREADS)
+norm_final_kernel(const double *__restrict__ partial, int64_t count, double max_norm, float *__restrict__ out)
+{
+    __shared__ double part[FINAL_THREADS / WAVE];
+    double acc[4] = {0.0, 0.0, 0.0, 0.0};
+    for (int64_t i = threadIdx.x; i < count; i += 4 * FINAL_THREADS) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (i + u * FINAL_THREADS < count) acc[u] += partial[i + u * FINAL_THREADS];
+    }
+    const double s = workgroup_sum<FINAL_THREADS>((acc[0] + acc[1]) + (acc[2] + acc[3]), part);
+    if (threadIdx.x == 0) write_norm(s, max_norm, out);
+}
+
+// chunks of all tensors, -1 if an argument is invalid
+int64_t total_chunks(const int64_t *numels, int64_t count)
+{
+    if (count < 0 || (count > 0 && numels == nullptr)) return -1;
+    int64_t chunks = 0;
+    for (int64_t j = 0; j < count; ++j) {
+        if (numels[j] < 0 || numels[j] > NORM_MAX_NUMEL) return -1;
+        chunks += (numels[j] + NORM_CHUNK - 1) / NORM_CHUNK;
+        if (chunks > int64_t(1) << 40) return -1;
+    }
+    return chunks;
+}
+
+// One workgroup takes the whole call: a launch and its gap (about 4 us) against up to four chunks one after the other (a
+// microsecond or so each).
+bool norm_small(int64_t tensors, int64_t chunks) { return tensors <= NORM_TENSORS && chunks <= 4; }
+
+int64_t nonempty(const int64_t *numels, int64_t count)
+{
+    int64_t n = 0;
+    for (int64_t j = 0; j < count; ++j) n += numels[j] > 0;
+    return n;
+}
+
+}  // namespace
+}  // namespace dropit
+
+using namespace dropit;
+
+extern "C" size_t dropit_grad_norm_workspace_bytes(const int64_t *numels, int64_t count)
+{
+    const int64_t chunks = total_chunks(numels, count);
+    if (chunks <= 0 || norm_small(nonempty(numels, count), chunks)) return 0;
+    return size_t(chunks) * sizeof(double);
+}
+
+extern "C" dropit_status dropit_grad_norm(const void *const *grads, const int64_t *numels, const int32_t *dtypes, int64_t count,
+                                          double max_norm, float *out, void *workspace, size_t workspace_bytes,
+                                          void *hip_stream)
+{
+    const int64_t chunks = total_chunks(numels, count);
+    if (chunks < 0 || (count > 0 && (grads == nullptr || dtypes == nullptr)) || !(max_norm > 0.0)) return DROPIT_EINVAL;
+    if (out == nullptr || !aligned(out, 4)) return DROPIT_EINVAL;
+    for (int64_t j = 0; j < count; ++j) {
+        if (dtypes[j] != DROPIT_F32 && dtypes[j] != DROPIT_BF16) return DROPIT_EINVAL;
+        if (numels[j] > 0 && (grads[j] == nullptr || !aligned(grads[j], dtypes[j] == DROPIT_BF16 ? 2 : 4))) return DROPIT_EINVAL;
+    }
+    const bool small = norm_small(nonempty(numels, count), chunks);
+    if (!small) {
+        if (workspace == nullptr || !aligned(workspace, 256)) return DROPIT_EINVAL;
+        if (workspace_bytes < size_t(chunks) * sizeof(double)) return DROPIT_EWORKSPACE;
+    }
+    const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    double *partial = static_cast<double *>(workspace);
+    NormTable table;
+    table.count = 0;
+    uint32_t at = 0;                                   // chunks of the table
+    auto flush = [&]() {
+        if (table.count == 0) return;
+        norm_chunks_kernel<<<at, NORM_THREADS, 0, stream>>>(table, partial);
+        partial += at;
+        table.count = 0;
+        at = 0;
+    };
+    for (int64_t j = 0; j < count; ++j) {
+        if (numels[j] == 0) continue;
+        const uint32_t need = uint32_t((numels[j] + NORM_CHUNK - 1) / NORM_CHUNK);
+        if (table.count == NORM_TENSORS || at + need > NORM_MAX_CHUNKS) flush();
+        table.g[table.count] = grads[j];
+        table.numel_bf16[table.count] = numels[j] * 2 + (dtypes[j] == DROPIT_BF16);
+        table.first[table.count] = at;
+        ++table.count;
+        at += need;
+    }
+    if (small) {
+        norm_small_kernel<<<1, NORM_THREADS, 0, stream>>>(table, at, max_norm, out);
+        return launch_status();
+    }
+    flush();
+    norm_final_kernel<<<1, FINAL_THREADS, 0, stream>>>(static_cast<const double *>(workspace), chunks, max_norm, out);
+    return launch_status();
+}
