@@ -20,6 +20,49 @@ extern "C" {
 #endif
 
 /*
+ * Gated projection of a feed-forward block: the gate and the up projection of every token, the activation and
+ * the product, in one pass.  With W [2 * hidden, c_in] (gate rows first), bias [2 * hidden] or NULL:
+ *     pre = x W^T + bias                                          [tokens, 2 * hidden], sums in fp32
+ *     h   = act(pre[:, :hidden]) * pre[:, hidden:]                [tokens, hidden]
+ * h is computed from the unrounded fp32 pre and rounded once; pre, where it is asked for, is rounded once too.
+ *     DROPIT_ACT_SILU z / (1 + e^-z), DROPIT_ACT_GELU z * Phi(z), DROPIT_ACT_GELU_TANH its tanh form
+ *     z / 2 * (1 + tanh(sqrt(2 / pi) * (z + 0.044715 z^3))), DROPIT_ACT_RELU max(z, 0), DROPIT_ACT_SIGMOID 1 / (1 + e^-z)
+ * bf16 evaluates them with the hardware's exponential and reciprocal (a relative 2^-20 or so; Phi by formula 7.1.26 of
+ * Abramowitz and Stegun, off by at most 1.5e-7), fp32 with the fp32 math library.
+ *
+ * x [tokens, c_in], w, bias, h, pre: device, row-major, type dt, 16-byte aligned; pre may be NULL (inference).
+ * 0 <= tokens < 2^31, 1 <= c_in <= 2^28, 1 <= hidden <= 2^27, and ceil(tokens / 64) times the larger of ceil(hidden / 64) and
+ * ceil(c_in / 128) at most 2^23.  Row offsets are 64-bit: none of the tensors is limited to 2^31 elements.
+ */
+typedef DROPIT_ENUM(dropit_act) {
+    DROPIT_ACT_SILU = 0,
+    DROPIT_ACT_GELU = 1,
+    DROPIT_ACT_GELU_TANH = 2,
+    DROPIT_ACT_RELU = 3,
+    DROPIT_ACT_SIGMOID = 4
+} dropit_act;
+
+size_t dropit_gated_forward_workspace_bytes(int64_t tokens, int64_t c_in, int64_t hidden, dropit_dtype dt);
+dropit_status dropit_gated_forward(const void *x, int64_t tokens, int64_t c_in, dropit_dtype dt, const void *w, const void *bias,
+                                   int64_t hidden, dropit_act act, void *h, void *pre, void *workspace,
+                                   size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Its backward pass.  With g = pre[:, :hidden], u = pre[:, hidden:]:
+ *     dpre  = [ dh * u * act'(g) | dh * act(g) ]                  [tokens, 2 * hidden], type dt
+ *     dx    = dpre W                                              [tokens, c_in], type dt, sums in fp32; may be NULL
+ *     dbias = sum of dpre over the tokens, before its rounding    [2 * hidden], fp32; may be NULL
+ * dx is computed from the rounded dpre.  The weight gradient dpre^T R(a^) is dropit_weight_grad's, with dY = dpre and
+ * c_out = 2 * hidden.  act'(0) of ReLU is 0.  The workspace query takes need_dx and need_dbias as 0 or 1.
+ * dh [tokens, hidden]; sizes, alignment and types as above.  dpre must not overlap pre.
+ */
+size_t dropit_gated_backward_workspace_bytes(int64_t tokens, int64_t c_in, int64_t hidden, dropit_dtype dt, int need_dx,
+                                             int need_dbias);
+dropit_status dropit_gated_backward(const void *dh, const void *pre, int64_t tokens, int64_t c_in, dropit_dtype dt,
+                                    const void *w, int64_t hidden, dropit_act act, void *dpre, void *dx, float *dbias,
+                                    void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
  * AdamW over many tensors at once.  For every element, with t the step (1 for the first) and s the value at
  * `grad_scale` (1 if NULL), in fp32, each operation rounded by itself (no fused multiply-adds):
  *     g = s * grad

@@ -31,5 +31,7 @@ from .binding import (  # noqa: F401
 from .layers import (  # noqa: F401
     adamw,
     adamw_unpack,
+    gated_backward,
+    gated_forward,
     grad_norm,
 )

@@ -98,6 +98,14 @@ def lib() -> ctypes.CDLL:
         L.dropit_weight_grad.restype = i32
         L.dropit_weight_grad.argtypes = [vp, vp, i64, p64, i32, i32, vp, i64, pconv, vp, vp, sz, vp]
         # dropit_layers.h (marshalled in layers.py)
+        L.dropit_gated_forward_workspace_bytes.restype = sz
+        L.dropit_gated_forward_workspace_bytes.argtypes = [i64, i64, i64, i32]
+        L.dropit_gated_forward.restype = i32
+        L.dropit_gated_forward.argtypes = [vp, i64, i64, i32, vp, vp, i64, i32, vp, vp, vp, sz, vp]
+        L.dropit_gated_backward_workspace_bytes.restype = sz
+        L.dropit_gated_backward_workspace_bytes.argtypes = [i64, i64, i64, i32, i32, i32]
+        L.dropit_gated_backward.restype = i32
+        L.dropit_gated_backward.argtypes = [vp, vp, i64, i64, i32, vp, i64, i32, vp, vp, vp, vp, sz, vp]
         L.dropit_adamw.restype = i32
         L.dropit_adamw.argtypes = [vp, i64, i32, i32, i32, vp, vp]
         L.dropit_adamw_unpack.restype = i32

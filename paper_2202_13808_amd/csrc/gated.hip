@@ -1,0 +1,505 @@
+// The gated projection of a feed-forward block and its backward pass (the formulas stand in dropit_layers.h): entry
+// points, the product that takes every size and type, and the element-wise part of the backward pass.
+//
+// Both products sum over a row of the token operand: the forward pass multiplies x [tokens, c_in] by W's gate and up rows,
+// the input gradient dpre [tokens, 2 * hidden] by W's columns.  The weights are the matrix instruction's row operand, so a
+// lane holds four consecutive output columns of one token.  In the forward pass a wavefront's row blocks come in pairs, a
+// gate block and the up block of the same columns, so the activation and the product happen in the accumulators.
+#include <algorithm>
+
+#include "common.hpp"
+#include "dropit_layers.h"
+#include "gated_act.hpp"
+#include "gated_internal.hpp"
+
+namespace dropit {
+namespace {
+
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+
+template <bool BF16> struct Elem { using type = float; static constexpr int PER16 = 4; };
+template <> struct Elem<true> { using type = uint16_t; static constexpr int PER16 = 8; };
+
+template <bool BF16> __device__ inline float load_one(const void *p, int64_t i)
+{
+    if constexpr (BF16) return __uint_as_float(uint32_t(static_cast<const uint16_t *>(p)[i]) << 16);
+    else return static_cast<const float *>(p)[i];
+}
+template <bool BF16> __device__ inline void store_one(void *p, int64_t i, float v)
+{
+    if constexpr (BF16) static_cast<__bf16 *>(p)[i] = static_cast<__bf16>(v);
+    else static_cast<float *>(p)[i] = v;
+}
+
+// ---------------------------------------------------------------------------
+// The product for every size and type: tiles of 64 tokens by 128 rows of the weight operand, four wavefronts of 64 x 32.
+// fp32 runs on the fp32 matrix instructions.  Rows whose length is no multiple of 16 bytes load element by element.
+// Few tiles: the sum is cut into slices, whose partial sums finish_kernel adds in ascending order.
+constexpr int GEN_THREADS = 256, GEN_ROWS = 128, GEN_TOKENS = 64, GEN_K = 32;
+
+struct GenArgs {
+    const void *w, *x;          // weight operand; token operand [tokens][K]
+    int64_t tokens;
+    int hidden, c_in;
+    int K;                      // forward: c_in, backward: 2 * hidden
+    int act;
+    const void *bias;
+    void *out, *pre;            // forward: h and pre; backward: dx
+    float *partial;             // [splits][tokens][width], or null: width = 2 * hidden (forward) or c_in (backward)
+    int splits, row_tiles;
+};
+
+// sixteen bytes of row `row` of a K-contiguous operand from element k on, zeros past the end
+template <bool BF16, bool VEC>
+__device__ inline u32x4 load_unit(const void *base, int64_t row, int64_t pitch, int k, int end)
+{
+    constexpr int PER = Elem<BF16>::PER16;
+    const auto *p = static_cast<const typename Elem<BF16>::type *>(base) + row * pitch + k;
+    if (VEC && k + PER <= end) return *reinterpret_cast<const u32x4 *>(p);
+    u32x4 r = {0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int e = 0; e < PER; ++e)
+        if (k + e < end) {
+            if constexpr (BF16) r[e >> 1] |= uint32_t(p[e]) << (16 * (e & 1));
+            else r[e] = __float_as_uint(p[e]);
+        }
+    return r;
+}
+
+template <bool BF16, bool FORWARD, bool VEC>
+__global__ void __launch_bounds__(GEN_THREADS)
+gated_product_kernel(const GenArgs a)
+{
+    constexpr int ES = BF16 ? 2 : 4, PER = Elem<BF16>::PER16;
+    constexpr int UNITS = GEN_K / PER;                              // 16-byte units of a tile row
+    constexpr int PITCH = GEN_K * ES + 16;                          // bytes of an LDS row: the pad spreads the rows over the banks
+    constexpr int A_LOADS = GEN_ROWS * UNITS / GEN_THREADS, B_LOADS = GEN_TOKENS * UNITS / GEN_THREADS;
+    __shared__ __attribute__((aligned(16))) char tile[2][(GEN_ROWS + GEN_TOKENS) * PITCH];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int wm = wave >> 1, wn = wave & 1;
+    const int rt = int(blockIdx.x % unsigned(a.row_tiles));
+    const int64_t t0 = int64_t(blockIdx.x / unsigned(a.row_tiles)) * GEN_TOKENS;
+    const int split = blockIdx.y;
+    const int r0 = rt * (FORWARD ? GEN_ROWS / 2 : GEN_ROWS);        // first output column of the tile
+    const int steps_all = (a.K + GEN_K - 1) / GEN_K;
+    const int s0 = int(int64_t(steps_all) * split / a.splits), s1 = int(int64_t(steps_all) * (split + 1) / a.splits);
+
+    // weight row of the tile's row R: forward, wavefront row R / 64 takes 32 gate rows and the 32 up rows of the same columns
+    auto weight_row = [&](int R) -> int64_t {
+        const int n = min(r0 + (R >> 6) * 32 + (R & 31), a.hidden - 1);
+        return (R & 32) ? int64_t(a.hidden) + n : n;
+    };
+    u32x4 ra[A_LOADS], rb[B_LOADS];
+    auto load = [&](int s) {
+        const int k0 = s * GEN_K;
+#pragma unroll
+        for (int i = 0; i < A_LOADS; ++i) {
+            const int unit = i * GEN_THREADS + tid;
+            if constexpr (FORWARD) {
+                ra[i] = load_unit<BF16, VEC>(a.w, weight_row(unit / UNITS), a.c_in, k0 + unit % UNITS * PER, a.K);
+            } else {                                                // W [K][c_in]: a unit is PER columns of one k
+                const int k = k0 + unit / (GEN_ROWS / PER), c = r0 + unit % (GEN_ROWS / PER) * PER;
+                ra[i] = k < a.K && c < a.c_in ? load_unit<BF16, VEC>(a.w, k, a.c_in, c, a.c_in) : u32x4{0u, 0u, 0u, 0u};
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < B_LOADS; ++i) {
+            const int unit = i * GEN_THREADS + tid;
+            rb[i] = load_unit<BF16, VEC>(a.x, min<int64_t>(t0 + unit / UNITS, a.tokens - 1), a.K, k0 + unit % UNITS * PER, a.K);
+        }
+    };
+    auto put = [&](char *to) {
+#pragma unroll
+        for (int i = 0; i < A_LOADS; ++i) {
+            const int unit = i * GEN_THREADS + tid;
+            if constexpr (FORWARD) {
+                *reinterpret_cast<u32x4 *>(to + unit / UNITS * PITCH + unit % UNITS * 16) = ra[i];
+            } else {
+                const int k = unit / (GEN_ROWS / PER), c = unit % (GEN_ROWS / PER) * PER;
+#pragma unroll
+                for (int e = 0; e < PER; ++e) {
+                    char *at = to + (c + e) * PITCH + k * ES;
+                    if constexpr (BF16) *reinterpret_cast<uint16_t *>(at) = uint16_t(ra[i][e >> 1] >> (16 * (e & 1)));
+                    else *reinterpret_cast<uint32_t *>(at) = ra[i][e];
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < B_LOADS; ++i) {
+            const int unit = i * GEN_THREADS + tid;
+            *reinterpret_cast<u32x4 *>(to + (GEN_ROWS + unit / UNITS) * PITCH + unit % UNITS * 16) = rb[i];
+        }
+    };
+
+    f32x16 acc[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[i][e] = 0.f;
+    if (s0 < s1) load(s0);
+    for (int s = s0; s < s1; ++s) {
+        char *cur = tile[(s - s0) & 1];
+        put(cur);
+        __syncthreads();                                            // (the other tile's readers passed the barrier before)
+        if (s + 1 < s1) load(s + 1);
+        const char *wa = cur + (wm * 64 + (lane & 31)) * PITCH, *xb = cur + (GEN_ROWS + wn * 32 + (lane & 31)) * PITCH;
+        if constexpr (BF16) {
+#pragma unroll
+            for (int kk = 0; kk < GEN_K / 16; ++kk) {
+                const int at = kk * 32 + (lane >> 5) * 16;
+                const bf16x8 b = *reinterpret_cast<const bf16x8 *>(xb + at);
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(wa + i * 32 * PITCH + at), b, acc[i], 0, 0, 0);
+            }
+        } else {
+            // an instruction takes one k from each half of the wavefront: k = 8 kk + e and 8 kk + 4 + e
+#pragma unroll
+            for (int kk = 0; kk < GEN_K / 8; ++kk) {
+                const int at = kk * 32 + (lane >> 5) * 16;
+                const f32x4 b = *reinterpret_cast<const f32x4 *>(xb + at);
+                f32x4 w[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) w[i] = *reinterpret_cast<const f32x4 *>(wa + i * 32 * PITCH + at);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) acc[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(w[i][e], b[e], acc[i], 0, 0, 0);
+            }
+        }
+    }
+    // lane l holds token l % 32 and, in register 4 q + e, row 8 q + 4 (l / 32) + e of each 32 x 32 block
+    const int64_t t = t0 + wn * 32 + (lane & 31);
+    if (t >= a.tokens) return;
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int m = q * 8 + (lane >> 5) * 4 + e;
+            if constexpr (FORWARD) {
+                const int n = r0 + wm * 32 + m;
+                if (n >= a.hidden) continue;
+                float g = acc[0][q * 4 + e], u = acc[1][q * 4 + e];
+                if (a.partial != nullptr) {
+                    float *to = a.partial + (int64_t(split) * a.tokens + t) * 2 * a.hidden;
+                    to[n] = g;
+                    to[a.hidden + n] = u;
+                    continue;
+                }
+                if (a.bias != nullptr) {
+                    g += load_one<BF16>(a.bias, n);
+                    u += load_one<BF16>(a.bias, int64_t(a.hidden) + n);
+                }
+                store_one<BF16>(a.out, t * a.hidden + n, activation<BF16>(g, a.act) * u);
+                if (a.pre != nullptr) {
+                    store_one<BF16>(a.pre, t * 2 * a.hidden + n, g);
+                    store_one<BF16>(a.pre, t * 2 * a.hidden + a.hidden + n, u);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int c = r0 + wm * 64 + i * 32 + m;
+                    if (c >= a.c_in) continue;
+                    if (a.partial != nullptr) a.partial[(int64_t(split) * a.tokens + t) * a.c_in + c] = acc[i][q * 4 + e];
+                    else store_one<BF16>(a.out, t * a.c_in + c, acc[i][q * 4 + e]);
+                }
+            }
+        }
+}
+
+// Adds the slices' partial sums in ascending order and finishes: bias, activation and product, or the rounding of dx.
+template <bool BF16, bool FORWARD>
+__global__ void __launch_bounds__(256)
+gated_finish_kernel(const GenArgs a)
+{
+    const int width = FORWARD ? a.hidden : a.c_in;
+    const int64_t total = a.tokens * width;
+    const int64_t slice = a.tokens * (FORWARD ? 2 * int64_t(a.hidden) : a.c_in);
+    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < total; i += int64_t(gridDim.x) * 256) {
+        const int64_t t = i / width, n = i - t * width;
+        if constexpr (FORWARD) {
+            const float *p = a.partial + t * 2 * a.hidden + n;
+            float g = 0.f, u = 0.f;
+            for (int s = 0; s < a.splits; ++s) {
+                g += p[s * slice];
+                u += p[s * slice + a.hidden];
+            }
+            if (a.bias != nullptr) {
+                g += load_one<BF16>(a.bias, n);
+                u += load_one<BF16>(a.bias, int64_t(a.hidden) + n);
+            }
+            store_one<BF16>(a.out, i, activation<BF16>(g, a.act) * u);
+            if (a.pre != nullptr) {
+                store_one<BF16>(a.pre, t * 2 * a.hidden + n, g);
+                store_one<BF16>(a.pre, t * 2 * a.hidden + a.hidden + n, u);
+            }
+        } else {
+            const float *p = a.partial + i;
+            float v = 0.f;
+            for (int s = 0; s < a.splits; ++s) v += p[s * slice];
+            store_one<BF16>(a.out, i, v);
+        }
+    }
+}
+
+// Slices of the sum: enough workgroups for two on each of 256 compute units, at least eight steps of 32 in a slice (below
+// that a slice is mostly its own start and end).
+int gen_splits(int64_t tokens, int rows, int per_tile, int64_t K)
+{
+    const int64_t tiles = (tokens + GEN_TOKENS - 1) / GEN_TOKENS * ((rows + per_tile - 1) / per_tile);
+    const int64_t steps = (K + GEN_K - 1) / GEN_K;
+    return int(std::max<int64_t>(1, std::min<int64_t>(512 / tiles, steps / 8)));
+}
+
+template <bool BF16, bool FORWARD>
+dropit_status launch_generic(GenArgs a, hipStream_t stream)
+{
+    constexpr int per_tile = FORWARD ? GEN_ROWS / 2 : GEN_ROWS;
+    const int rows = FORWARD ? a.hidden : a.c_in;
+    a.row_tiles = (rows + per_tile - 1) / per_tile;
+    a.splits = gen_splits(a.tokens, rows, per_tile, a.K);
+    if (a.splits == 1) a.partial = nullptr;
+    const int64_t tiles = (a.tokens + GEN_TOKENS - 1) / GEN_TOKENS * a.row_tiles;
+    const dim3 grid(static_cast<uint32_t>(tiles), a.splits);
+    // whole rows in 16-byte units: both operands' row lengths allow it
+    const bool vec = a.c_in % Elem<BF16>::PER16 == 0 && a.K % Elem<BF16>::PER16 == 0;
+    if (vec) gated_product_kernel<BF16, FORWARD, true><<<grid, GEN_THREADS, 0, stream>>>(a);
+    else gated_product_kernel<BF16, FORWARD, false><<<grid, GEN_THREADS, 0, stream>>>(a);
+    if (a.splits > 1) {
+        const int64_t blocks = (a.tokens * rows + 255) / 256;
+        gated_finish_kernel<BF16, FORWARD><<<static_cast<uint32_t>(std::min<int64_t>(blocks, 1 << 16)), 256, 0, stream>>>(a);
+    }
+    return launch_status();
+}
+
+// ---------------------------------------------------------------------------
+// dpre from dh and pre, and the partial column sums for dbias.  A thread takes 8 (bf16) or 4 (fp32) gate columns, the up
+// columns beside them and every fourth row of a block of rows; the four row groups' sums meet in LDS.
+constexpr int SLOPE_LANES = 64, SLOPE_GROUPS = 4, SLOPE_ROWS = 64;
+
+template <bool BF16, bool VEC>
+__global__ void __launch_bounds__(SLOPE_LANES * SLOPE_GROUPS)
+gated_slope_kernel(const void *__restrict__ dh, const void *__restrict__ pre, int64_t tokens, int hidden, int act,
+                   void *__restrict__ dpre, float *__restrict__ partial /* [row blocks][2 * hidden] or null */)
+{
+    constexpr int PER = VEC ? Elem<BF16>::PER16 : 1;
+    __shared__ float red[SLOPE_GROUPS][SLOPE_LANES * PER * 2];
+    const int lane = threadIdx.x % SLOPE_LANES, group = threadIdx.x / SLOPE_LANES;
+    const int n = int(blockIdx.x * SLOPE_LANES + lane) * PER;
+    const int64_t t0 = int64_t(blockIdx.y) * SLOPE_ROWS, t1 = min<int64_t>(t0 + SLOPE_ROWS, tokens);
+    float sg[PER], su[PER];
+#pragma unroll
+    for (int e = 0; e < PER; ++e) sg[e] = su[e] = 0.f;
+    if (n < hidden) {
+#pragma unroll 2
+        for (int64_t t = t0 + group; t < t1; t += SLOPE_GROUPS) {
+            const int64_t ih = t * hidden + n, ig = t * 2 * hidden + n, iu = ig + hidden;
+            float d[PER], g[PER], u[PER];
+            if constexpr (VEC) {
+                using T = typename Elem<BF16>::type;
+                const u32x4 rd = *reinterpret_cast<const u32x4 *>(static_cast<const T *>(dh) + ih);
+                const u32x4 rg = *reinterpret_cast<const u32x4 *>(static_cast<const T *>(pre) + ig);
+                const u32x4 ru = *reinterpret_cast<const u32x4 *>(static_cast<const T *>(pre) + iu);
+#pragma unroll
+                for (int e = 0; e < PER; ++e) {
+                    if constexpr (BF16) {
+                        d[e] = __uint_as_float((e & 1) ? rd[e >> 1] & 0xffff0000u : rd[e >> 1] << 16);
+                        g[e] = __uint_as_float((e & 1) ? rg[e >> 1] & 0xffff0000u : rg[e >> 1] << 16);
+                        u[e] = __uint_as_float((e & 1) ? ru[e >> 1] & 0xffff0000u : ru[e >> 1] << 16);
+                    } else {
+                        d[e] = __uint_as_float(rd[e]);
+                        g[e] = __uint_as_float(rg[e]);
+                        u[e] = __uint_as_float(ru[e]);
+                    }
+                }
+            } else {
+                d[0] = load_one<BF16>(dh, ih);
+                g[0] = load_one<BF16>(pre, ig);
+                u[0] = load_one<BF16>(pre, iu);
+            }
+#pragma unroll
+            for (int e = 0; e < PER; ++e) {
+                float slope;
+                const float value = activation_slope<BF16>(g[e], act, slope);
+                g[e] = d[e] * u[e] * slope;
+                u[e] = d[e] * value;
+                sg[e] += g[e];
+                su[e] += u[e];
+            }
+            if constexpr (VEC && BF16) {
+                bf16x8 og, ou;
+#pragma unroll
+                for (int e = 0; e < PER; ++e) {
+                    og[e] = static_cast<__bf16>(g[e]);
+                    ou[e] = static_cast<__bf16>(u[e]);
+                }
+                *reinterpret_cast<bf16x8 *>(static_cast<uint16_t *>(dpre) + ig) = og;
+                *reinterpret_cast<bf16x8 *>(static_cast<uint16_t *>(dpre) + iu) = ou;
+            } else if constexpr (VEC) {
+                *reinterpret_cast<f32x4 *>(static_cast<float *>(dpre) + ig) = f32x4{g[0], g[1], g[2], g[3]};
+                *reinterpret_cast<f32x4 *>(static_cast<float *>(dpre) + iu) = f32x4{u[0], u[1], u[2], u[3]};
+            } else {
+                store_one<BF16>(dpre, ig, g[0]);
+                store_one<BF16>(dpre, iu, u[0]);
+            }
+        }
+    }
+    if (partial == nullptr) return;                    // (the same for every thread)
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+        red[group][lane * PER + e] = sg[e];
+        red[group][SLOPE_LANES * PER + lane * PER + e] = su[e];
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < SLOPE_LANES * PER * 2; i += SLOPE_LANES * SLOPE_GROUPS) {
+        const bool up = i >= SLOPE_LANES * PER;
+        const int col = int(blockIdx.x) * SLOPE_LANES * PER + (up ? i - SLOPE_LANES * PER : i);
+        if (col < hidden)
+            partial[int64_t(blockIdx.y) * 2 * hidden + (up ? hidden : 0) + col] = (red[0][i] + red[1][i]) + (red[2][i] + red[3][i]);
+    }
+}
+
+// dbias: the row blocks' partial sums of a column, 16 threads a column, in a fixed order
+__global__ void __launch_bounds__(256)
+gated_bias_kernel(const float *__restrict__ partial, int64_t blocks, int64_t width, float *__restrict__ dbias)
+{
+    __shared__ float red[16][17];
+    const int col = threadIdx.x & 15, part = threadIdx.x >> 4;
+    const int64_t n = int64_t(blockIdx.x) * 16 + col;
+    float s = 0.f;
+    if (n < width)
+        for (int64_t b = part; b < blocks; b += 16) s += partial[b * width + n];
+    red[part][col] = s;
+    __syncthreads();
+    if (part != 0 || n >= width) return;
+#pragma unroll
+    for (int q = 1; q < 16; ++q) s += red[q][col];
+    dbias[n] = s;
+}
+
+int64_t row_blocks(int64_t tokens) { return (tokens + SLOPE_ROWS - 1) / SLOPE_ROWS; }
+
+bool valid_sizes(int64_t tokens, int64_t c_in, int64_t hidden, dropit_dtype dt)
+{
+    if (tokens < 0 || tokens > INT32_MAX || c_in < 1 || c_in > 1 << 28 || hidden < 1 || hidden > 1 << 27) return false;
+    if (dt != DROPIT_F32 && dt != DROPIT_BF16) return false;
+    // a launch has fewer than 2^32 threads
+    const int64_t across = std::max((hidden + GEN_ROWS / 2 - 1) / (GEN_ROWS / 2), (c_in + GEN_ROWS - 1) / GEN_ROWS);
+    return (tokens + GEN_TOKENS - 1) / GEN_TOKENS * across <= 1 << 23;
+}
+
+size_t forward_bytes(int64_t tokens, int64_t c_in, int64_t hidden)
+{
+    const int splits = tokens == 0 ? 1 : gen_splits(tokens, int(hidden), GEN_ROWS / 2, c_in);
+    return splits == 1 ? 0 : size_t(splits) * tokens * 2 * hidden * sizeof(float);
+}
+
+size_t dx_bytes(int64_t tokens, int64_t c_in, int64_t hidden)
+{
+    const int splits = tokens == 0 ? 1 : gen_splits(tokens, int(c_in), GEN_ROWS, 2 * hidden);
+    return splits == 1 ? 0 : size_t(splits) * tokens * c_in * sizeof(float);
+}
+
+}  // namespace
+}  // namespace dropit
+
+using namespace dropit;
+
+extern "C" size_t dropit_gated_forward_workspace_bytes(int64_t tokens, int64_t c_in, int64_t hidden, dropit_dtype dt)
+{
+    if (!valid_sizes(tokens, c_in, hidden, dt)) return 0;
+    return forward_bytes(tokens, c_in, hidden);
+}
+
+extern "C" dropit_status dropit_gated_forward(const void *x, int64_t tokens, int64_t c_in, dropit_dtype dt, const void *w,
+                                              const void *bias, int64_t hidden, dropit_act act, void *h, void *pre,
+                                              void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    if (!valid_sizes(tokens, c_in, hidden, dt) || act < DROPIT_ACT_SILU || act > DROPIT_ACT_SIGMOID) return DROPIT_EINVAL;
+    if (tokens == 0) return DROPIT_OK;
+    if (!x || !w || !h || !aligned(x, 16) || !aligned(w, 16) || !aligned(h, 16) || !aligned(bias, 16) || !aligned(pre, 16))
+        return DROPIT_EINVAL;
+    const size_t need = forward_bytes(tokens, c_in, hidden);
+    if (need > 0 && (workspace == nullptr || !aligned(workspace, 256))) return DROPIT_EINVAL;
+    if (workspace_bytes < need) return DROPIT_EWORKSPACE;
+    const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    GenArgs a{};
+    a.w = w;
+    a.x = x;
+    a.tokens = tokens;
+    a.hidden = int(hidden);
+    a.c_in = int(c_in);
+    a.K = int(c_in);
+    a.act = act;
+    a.bias = bias;
+    a.out = h;
+    a.pre = pre;
+    a.partial = static_cast<float *>(workspace);
+    return dt == DROPIT_BF16 ? launch_generic<true, true>(a, stream) : launch_generic<false, true>(a, stream);
+}
+
+extern "C" size_t dropit_gated_backward_workspace_bytes(int64_t tokens, int64_t c_in, int64_t hidden, dropit_dtype dt, int need_dx,
+                                                        int need_dbias)
+{
+    if (!valid_sizes(tokens, c_in, hidden, dt)) return 0;
+    size_t need = need_dx ? dx_bytes(tokens, c_in, hidden) : 0;
+    if (need_dbias) need = std::max(need, size_t(row_blocks(tokens)) * 2 * hidden * sizeof(float));
+    return need;
+}
+
+extern "C" dropit_status dropit_gated_backward(const void *dh, const void *pre, int64_t tokens, int64_t c_in, dropit_dtype dt,
+                                               const void *w, int64_t hidden, dropit_act act, void *dpre, void *dx, float *dbias,
+                                               void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    if (!valid_sizes(tokens, c_in, hidden, dt) || act < DROPIT_ACT_SILU || act > DROPIT_ACT_SIGMOID) return DROPIT_EINVAL;
+    if (!aligned(dbias, 16)) return DROPIT_EINVAL;
+    if (tokens > 0 && (!dh || !pre || !dpre || (dx && !w) || !aligned(dh, 16) || !aligned(pre, 16) || !aligned(dpre, 16) ||
+                       !aligned(w, 16) || !aligned(dx, 16)))
+        return DROPIT_EINVAL;
+    const size_t need = dropit_gated_backward_workspace_bytes(tokens, c_in, hidden, dt, dx != nullptr, dbias != nullptr);
+    if (need > 0 && (workspace == nullptr || !aligned(workspace, 256))) return DROPIT_EINVAL;
+    if (workspace_bytes < need) return DROPIT_EWORKSPACE;
+    const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    const bool bf16 = dt == DROPIT_BF16;
+    // the partial column sums and, when those are added, dx's slices share the workspace, one after the other
+    float *partial = dbias != nullptr ? static_cast<float *>(workspace) : nullptr;
+    if (tokens > 0) {
+        const bool vec = hidden % (bf16 ? 8 : 4) == 0;
+        const int64_t cols = vec ? hidden / (bf16 ? 8 : 4) : hidden;
+        const int64_t strips = (cols + SLOPE_LANES - 1) / SLOPE_LANES;
+        // the grid's second dimension holds 65535 row blocks: more tokens go in several launches
+        for (int64_t b0 = 0; b0 < row_blocks(tokens); b0 += 65535) {
+            const int64_t first = b0 * SLOPE_ROWS, some = std::min<int64_t>(tokens - first, int64_t(65535) * SLOPE_ROWS);
+            const dim3 grid(static_cast<uint32_t>(strips), static_cast<uint32_t>(row_blocks(some)));
+            const size_t es = bf16 ? 2 : 4;
+            const char *d = static_cast<const char *>(dh) + first * hidden * es;
+            const char *p = static_cast<const char *>(pre) + first * 2 * hidden * es;
+            char *o = static_cast<char *>(dpre) + first * 2 * hidden * es;
+            float *part = partial != nullptr ? partial + b0 * 2 * hidden : nullptr;
+            auto launch = [&](auto kernel) {
+                kernel<<<grid, SLOPE_LANES * SLOPE_GROUPS, 0, stream>>>(d, p, some, int(hidden), act, o, part);
+            };
+            if (bf16 && vec) launch(gated_slope_kernel<true, true>);
+            else if (bf16) launch(gated_slope_kernel<true, false>);
+            else if (vec) launch(gated_slope_kernel<false, true>);
+            else launch(gated_slope_kernel<false, false>);
+        }
+    }
+    if (dbias != nullptr)
+        gated_bias_kernel<<<static_cast<uint32_t>((2 * hidden + 15) / 16), 256, 0, stream>>>(partial, row_blocks(tokens), 2 * hidden, dbias);
+    if (dx == nullptr || tokens == 0) return launch_status();
+    GenArgs a{};
+    a.w = w;
+    a.x = dpre;
+    a.tokens = tokens;
+    a.hidden = int(hidden);
+    a.c_in = int(c_in);
+    a.K = int(2 * hidden);
+    a.act = act;
+    a.out = dx;
+    a.partial = static_cast<float *>(workspace);
+    return bf16 ? launch_generic<true, false>(a, stream) : launch_generic<false, false>(a, stream);
+}

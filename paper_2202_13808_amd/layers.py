@@ -1,7 +1,7 @@
 """ctypes binding of the C ABI in ``include/dropit_layers.h`` -- marshalling and checks only.
 
-The operators that stand beside the dropped cache in a training step: the AdamW step over many tensors, the
-global gradient norm.  Functions have the names of the C entry points without the ``dropit_`` prefix; the
+The operators that stand beside the dropped cache in a training step: the gated projection of a feed-forward block
+and its backward pass, the AdamW step over many tensors, the global gradient norm.  Functions have the names of the C entry points without the ``dropit_`` prefix; the
 formulas stand in the header.
 """
 from __future__ import annotations
@@ -13,11 +13,106 @@ from typing import List, Optional, Sequence, Tuple, Union
 import numpy as np
 import torch
 
-from .binding import BF16, F32, _check, _on, _require_device, _stream_ptr, lib
+from .binding import BF16, F32, _check, _dtype_code, _on, _require_device, _stream_ptr, lib
 
 ADAMW_BLOCK = 256      # DROPIT_ADAMW_BLOCK: elements that share an offset of the 8-bit states
 
 _CODES = {torch.float32: F32, torch.bfloat16: BF16}
+
+
+ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "relu": 3, "sigmoid": 4}      # dropit_act
+
+
+def _act_code(act: str) -> int:
+    if act not in ACTIVATIONS:
+        raise ValueError("act must be one of %s, got %r" % (", ".join(ACTIVATIONS), act))
+    return ACTIVATIONS[act]
+
+
+def _gated_sizes(weight: torch.Tensor) -> Tuple[int, int]:
+    if weight.dim() != 2 or weight.shape[0] % 2 or weight.shape[0] == 0 or weight.shape[1] == 0:
+        raise ValueError("weight must be [2 * hidden, c_in], gate rows first, got %s" % (tuple(weight.shape),))
+    return weight.shape[0] // 2, weight.shape[1]
+
+
+def _like(t: Optional[torch.Tensor], shape, dtype: torch.dtype, device: torch.device, what: str) -> torch.Tensor:
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if t.dtype != dtype or t.numel() != math.prod(shape) or t.device != device:
+        raise ValueError("%s must hold %s elements of %s on %s" % (what, tuple(shape), dtype, device))
+    return t
+
+
+def _one_device(*tensors) -> None:
+    found = {t.device for t in tensors if t is not None}
+    if len(found) > 1:
+        raise ValueError("the tensors of a call must be on one device, got %s" % sorted(map(str, found)))
+
+
+def _area(workspace: Optional[torch.Tensor], need: int, device: torch.device) -> Tuple[Optional[int], int]:
+    if workspace is None:
+        if need == 0:
+            return None, 0
+        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def gated_forward(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, act: str = "silu",
+                  save: bool = False, h: Optional[torch.Tensor] = None, pre: Optional[torch.Tensor] = None,
+                  workspace: Optional[torch.Tensor] = None, stream=None):
+    """dropit_gated_forward: h = act(x Wg^T + bg) * (x Wu^T + bu) with ``weight`` = [Wg; Wu] of shape [2 * hidden, c_in]
+    and ``bias`` [2 * hidden]; ``x`` [..., c_in] gives h [..., hidden].  ``save`` returns (h, pre) with the
+    pre-activations [..., 2 * hidden] that ``gated_backward`` takes.  ``act``: silu, gelu, gelu_tanh, relu or sigmoid."""
+    _require_device(x, weight, bias, h, pre, workspace)
+    _one_device(x, weight, bias, h, pre, workspace)
+    code, hidden, c_in, act_code = _dtype_code(x.dtype), *_gated_sizes(weight), _act_code(act)
+    if weight.dtype != x.dtype or (bias is not None and (bias.dtype != x.dtype or bias.numel() != 2 * hidden)):
+        raise ValueError("weight and bias must have x's dtype, bias 2 * hidden = %d elements" % (2 * hidden))
+    if x.dim() < 1 or x.shape[-1] != c_in:
+        raise ValueError("x must be [..., %d], got %s" % (c_in, tuple(x.shape)))
+    lead, tokens = tuple(x.shape[:-1]), x.numel() // c_in
+    h = _like(h, lead + (hidden,), x.dtype, x.device, "h")
+    if save or pre is not None:
+        pre = _like(pre, lead + (2 * hidden,), x.dtype, x.device, "pre")
+    need = int(lib().dropit_gated_forward_workspace_bytes(tokens, c_in, hidden, code))
+    area, size = _area(workspace, need, x.device)
+    with _on(x.device):
+        _check(lib().dropit_gated_forward(x.data_ptr(), tokens, c_in, code, weight.data_ptr(),
+                                          bias.data_ptr() if bias is not None else None, hidden, act_code, h.data_ptr(),
+                                          pre.data_ptr() if pre is not None else None, area, size,
+                                          _stream_ptr(stream, x.device)))
+    return (h, pre) if pre is not None else h
+
+
+def gated_backward(dh: torch.Tensor, pre: torch.Tensor, weight: torch.Tensor, act: str = "silu", need_dx: bool = True,
+                   need_dbias: bool = False, dpre: Optional[torch.Tensor] = None, dx: Optional[torch.Tensor] = None,
+                   dbias: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None
+                   ) -> Tuple[torch.Tensor, Optional[torch.Tensor], Optional[torch.Tensor]]:
+    """dropit_gated_backward: (dpre [..., 2 * hidden], dx [..., c_in] or None, dbias [2 * hidden] float32 or None) from
+    dh [..., hidden] and what ``gated_forward`` saved.  The weight gradient is ``weight_grad`` of the cached x with
+    dY = dpre and c_out = 2 * hidden."""
+    _require_device(dh, pre, weight, dpre, dx, dbias, workspace)
+    _one_device(dh, pre, weight, dpre, dx, dbias, workspace)
+    code, hidden, c_in, act_code = _dtype_code(dh.dtype), *_gated_sizes(weight), _act_code(act)
+    if weight.dtype != dh.dtype or pre.dtype != dh.dtype:
+        raise ValueError("pre and weight must have dh's dtype")
+    if dh.dim() < 1 or dh.shape[-1] != hidden or tuple(pre.shape) != tuple(dh.shape[:-1]) + (2 * hidden,):
+        raise ValueError("dh must be [..., %d] and pre [..., %d], got %s and %s" % (hidden, 2 * hidden, tuple(dh.shape), tuple(pre.shape)))
+    lead, tokens = tuple(dh.shape[:-1]), dh.numel() // hidden
+    dpre = _like(dpre, lead + (2 * hidden,), dh.dtype, dh.device, "dpre")
+    need_dx, need_dbias = need_dx or dx is not None, need_dbias or dbias is not None
+    if need_dx:
+        dx = _like(dx, lead + (c_in,), dh.dtype, dh.device, "dx")
+    if need_dbias:
+        dbias = _like(dbias, (2 * hidden,), torch.float32, dh.device, "dbias")
+    need = int(lib().dropit_gated_backward_workspace_bytes(tokens, c_in, hidden, code, int(need_dx), int(need_dbias)))
+    area, size = _area(workspace, need, dh.device)
+    with _on(dh.device):
+        _check(lib().dropit_gated_backward(dh.data_ptr(), pre.data_ptr(), tokens, c_in, code, weight.data_ptr(), hidden, act_code,
+                                           dpre.data_ptr(), dx.data_ptr() if need_dx else None,
+                                           dbias.data_ptr() if need_dbias else None, area, size,
+                                           _stream_ptr(stream, dh.device)))
+    return dpre, dx if need_dx else None, dbias if need_dbias else None
 
 
 class _AdamwHyper(ctypes.Structure):

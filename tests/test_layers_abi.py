@@ -18,6 +18,8 @@ FAKE = 0x100000            # never dereferenced: validation fails first
 def test_library_exports_every_declared_symbol():
     text = re.sub(r"/\*.*?\*/", "", open(os.path.join(ROOT, "include", "dropit_layers.h")).read(), flags=re.S)
     names = set(re.findall(r"\b(dropit_[a-z_0-9]+)\s*\(", text))
+    assert {"dropit_gated_forward", "dropit_gated_forward_workspace_bytes", "dropit_gated_backward",
+            "dropit_gated_backward_workspace_bytes"} <= names
     assert {"dropit_adamw", "dropit_adamw_unpack", "dropit_grad_norm", "dropit_grad_norm_workspace_bytes"} <= names
     for name in names:
         assert hasattr(dropit.lib(), name), name
@@ -101,3 +103,46 @@ def test_python_entry_points_refuse_host_tensors_and_mismatches():
     with pytest.raises(ValueError):
         dropit.adamw_unpack(torch.zeros(3, dtype=torch.uint8), torch.zeros(1, dtype=torch.int16), True)
     dropit.adamw([], [], [], [], lr=1e-3, step=1)
+
+
+def test_gated_projection_refuses_bad_arguments_without_a_gpu():
+    L, big = dropit.lib(), 1 << 40
+
+    def forward(x=FAKE, t=10, c=16, dt=binding.BF16, w=FAKE, b=None, n=8, act=0, h=FAKE, pre=None, ws=FAKE, nbytes=big):
+        return L.dropit_gated_forward(x, t, c, dt, w, b, n, act, h, pre, ws, nbytes, None)
+
+    for kw in (dict(x=None), dict(w=None), dict(h=None), dict(x=FAKE + 8), dict(w=FAKE + 2), dict(h=FAKE + 4), dict(b=FAKE + 2),
+               dict(pre=FAKE + 8), dict(t=-1), dict(c=0), dict(n=0), dict(c=(1 << 28) + 1), dict(n=(1 << 27) + 1),
+               dict(t=1 << 31), dict(t=(1 << 31) - 1, n=1 << 20), dict(dt=2), dict(act=-1), dict(act=5)):
+        assert forward(**kw) == binding.EINVAL, kw
+    assert forward(t=0, x=None, w=None, h=None) == binding.OK
+    need = L.dropit_gated_forward_workspace_bytes(1, 4096, 64, binding.F32)
+    assert need > 0
+    assert forward(t=1, c=4096, n=64, dt=binding.F32, nbytes=need - 1) == binding.EWORKSPACE
+    assert forward(t=1, c=4096, n=64, dt=binding.F32, ws=None) == binding.EINVAL
+    assert forward(t=1, c=4096, n=64, dt=binding.F32, ws=FAKE + 16) == binding.EINVAL
+
+    def backward(dh=FAKE, pre=FAKE, t=10, c=16, dt=binding.BF16, w=FAKE, n=8, act=0, dpre=FAKE, dx=FAKE, db=FAKE, ws=FAKE, nbytes=big):
+        return L.dropit_gated_backward(dh, pre, t, c, dt, w, n, act, dpre, dx, db, ws, nbytes, None)
+
+    for kw in (dict(dh=None), dict(pre=None), dict(w=None), dict(dpre=None), dict(dh=FAKE + 2), dict(pre=FAKE + 8),
+               dict(dpre=FAKE + 8), dict(dx=FAKE + 8), dict(db=FAKE + 4), dict(w=FAKE + 4), dict(t=-1), dict(c=0), dict(n=0),
+               dict(dt=9), dict(act=7), dict(ws=None), dict(ws=FAKE + 64)):
+        assert backward(**kw) == binding.EINVAL, kw
+    assert backward(nbytes=16) == binding.EWORKSPACE
+    assert L.dropit_gated_backward_workspace_bytes(10, 16, 8, binding.BF16, 0, 0) == 0
+    assert L.dropit_gated_backward_workspace_bytes(10, 16, 8, binding.BF16, 0, 1) == 16 * 4
+    assert L.dropit_gated_backward_workspace_bytes(10, 0, 8, binding.BF16, 1, 1) == 0
+
+
+def test_gated_projection_in_python_refuses_host_tensors_and_mismatches():
+    x, w = torch.zeros(4, 8), torch.zeros(6, 8)
+    with pytest.raises(ValueError):
+        dropit.gated_forward(x, w)
+    with pytest.raises(ValueError):
+        dropit.gated_backward(torch.zeros(4, 3), torch.zeros(4, 6), w)
+    with pytest.raises(ValueError):
+        layers._act_code("tanh")
+    for bad in (torch.zeros(5, 8), torch.zeros(6), torch.zeros(0, 8), torch.zeros(6, 0)):
+        with pytest.raises(ValueError):
+            layers._gated_sizes(bad)
