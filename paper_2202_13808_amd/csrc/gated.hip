@@ -382,6 +382,22 @@ gated_bias_kernel(const float *__restrict__ partial, int64_t blocks, int64_t wid
 
 int64_t row_blocks(int64_t tokens) { return (tokens + SLOPE_ROWS - 1) / SLOPE_ROWS; }
 
+WideArgs wide_args(const GenArgs &g)
+{
+    WideArgs a{};
+    a.w = g.w;
+    a.x = g.x;
+    a.tokens = g.tokens;
+    a.hidden = g.hidden;
+    a.c_in = g.c_in;
+    a.K = g.K;
+    a.act = g.act;
+    a.bias = g.bias;
+    a.out = g.out;
+    a.pre = g.pre;
+    return a;
+}
+
 bool valid_sizes(int64_t tokens, int64_t c_in, int64_t hidden, dropit_dtype dt)
 {
     if (tokens < 0 || tokens > INT32_MAX || c_in < 1 || c_in > 1 << 28 || hidden < 1 || hidden > 1 << 27) return false;
@@ -391,14 +407,16 @@ bool valid_sizes(int64_t tokens, int64_t c_in, int64_t hidden, dropit_dtype dt)
     return (tokens + GEN_TOKENS - 1) / GEN_TOKENS * across <= 1 << 23;
 }
 
-size_t forward_bytes(int64_t tokens, int64_t c_in, int64_t hidden)
+size_t forward_bytes(int64_t tokens, int64_t c_in, int64_t hidden, dropit_dtype dt)
 {
+    if (dt == DROPIT_BF16 && gated_wide_takes(tokens, int(c_in), int(hidden), true)) return 0;
     const int splits = tokens == 0 ? 1 : gen_splits(tokens, int(hidden), GEN_ROWS / 2, c_in);
     return splits == 1 ? 0 : size_t(splits) * tokens * 2 * hidden * sizeof(float);
 }
 
-size_t dx_bytes(int64_t tokens, int64_t c_in, int64_t hidden)
+size_t dx_bytes(int64_t tokens, int64_t c_in, int64_t hidden, dropit_dtype dt)
 {
+    if (dt == DROPIT_BF16 && gated_wide_takes(tokens, int(c_in), int(hidden), false)) return 0;
     const int splits = tokens == 0 ? 1 : gen_splits(tokens, int(c_in), GEN_ROWS, 2 * hidden);
     return splits == 1 ? 0 : size_t(splits) * tokens * c_in * sizeof(float);
 }
@@ -411,7 +429,7 @@ using namespace dropit;
 extern "C" size_t dropit_gated_forward_workspace_bytes(int64_t tokens, int64_t c_in, int64_t hidden, dropit_dtype dt)
 {
     if (!valid_sizes(tokens, c_in, hidden, dt)) return 0;
-    return forward_bytes(tokens, c_in, hidden);
+    return forward_bytes(tokens, c_in, hidden, dt);
 }
 
 extern "C" dropit_status dropit_gated_forward(const void *x, int64_t tokens, int64_t c_in, dropit_dtype dt, const void *w,
@@ -422,7 +440,7 @@ extern "C" dropit_status dropit_gated_forward(const void *x, int64_t tokens, int
     if (tokens == 0) return DROPIT_OK;
     if (!x || !w || !h || !aligned(x, 16) || !aligned(w, 16) || !aligned(h, 16) || !aligned(bias, 16) || !aligned(pre, 16))
         return DROPIT_EINVAL;
-    const size_t need = forward_bytes(tokens, c_in, hidden);
+    const size_t need = forward_bytes(tokens, c_in, hidden, dt);
     if (need > 0 && (workspace == nullptr || !aligned(workspace, 256))) return DROPIT_EINVAL;
     if (workspace_bytes < need) return DROPIT_EWORKSPACE;
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
@@ -438,6 +456,7 @@ extern "C" dropit_status dropit_gated_forward(const void *x, int64_t tokens, int
     a.out = h;
     a.pre = pre;
     a.partial = static_cast<float *>(workspace);
+    if (dt == DROPIT_BF16 && gated_wide_takes(tokens, a.c_in, a.hidden, true)) return launch_gated_wide(wide_args(a), true, stream);
     return dt == DROPIT_BF16 ? launch_generic<true, true>(a, stream) : launch_generic<false, true>(a, stream);
 }
 
@@ -445,7 +464,7 @@ extern "C" size_t dropit_gated_backward_workspace_bytes(int64_t tokens, int64_t 
                                                         int need_dbias)
 {
     if (!valid_sizes(tokens, c_in, hidden, dt)) return 0;
-    size_t need = need_dx ? dx_bytes(tokens, c_in, hidden) : 0;
+    size_t need = need_dx ? dx_bytes(tokens, c_in, hidden, dt) : 0;
     if (need_dbias) need = std::max(need, size_t(row_blocks(tokens)) * 2 * hidden * sizeof(float));
     return need;
 }
@@ -501,5 +520,6 @@ extern "C" dropit_status dropit_gated_backward(const void *dh, const void *pre, 
     a.act = act;
     a.out = dx;
     a.partial = static_cast<float *>(workspace);
+    if (bf16 && gated_wide_takes(tokens, a.c_in, a.hidden, false)) return launch_gated_wide(wide_args(a), false, stream);
     return bf16 ? launch_generic<true, false>(a, stream) : launch_generic<false, false>(a, stream);
 }
