@@ -1,6 +1,8 @@
 // The activations of the gated projection and their slopes (internal header).
 #pragma once
 
+#include <type_traits>
+
 #include "common.hpp"
 #include "dropit_layers.h"
 
@@ -45,6 +47,22 @@ template <bool FAST> __device__ inline float activation(float z, int act)
     case DROPIT_ACT_GELU_TANH: return z * sigmoid_of<FAST>(2.f * TANH_K * (z + TANH_C * z * z * z));    // (1 + tanh y) / 2 = sigmoid(2 y)
     case DROPIT_ACT_RELU: return z < 0.f ? 0.f : z;    // (a NaN stays one)
     default: return sigmoid_of<FAST>(z);
+    }
+}
+
+// act over N values at once: one branch for all of them, and their exponentials and reciprocals in flight together
+template <bool FAST, int N> __device__ inline void activations(float (&z)[N], int act)
+{
+    auto each = [&](auto code) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) z[i] = activation<FAST>(z[i], decltype(code)::value);
+    };
+    switch (act) {
+    case DROPIT_ACT_SILU: return each(std::integral_constant<int, DROPIT_ACT_SILU>{});
+    case DROPIT_ACT_GELU: return each(std::integral_constant<int, DROPIT_ACT_GELU>{});
+    case DROPIT_ACT_GELU_TANH: return each(std::integral_constant<int, DROPIT_ACT_GELU_TANH>{});
+    case DROPIT_ACT_RELU: return each(std::integral_constant<int, DROPIT_ACT_RELU>{});
+    default: return each(std::integral_constant<int, DROPIT_ACT_SIGMOID>{});
     }
 }
 

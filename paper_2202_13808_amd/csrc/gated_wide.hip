@@ -1,21 +1,32 @@
 // The gated projection's products on wide tiles: bf16, many tokens (gated.hip takes every other size and type).
 //
-// A workgroup of eight wavefronts computes 256 rows of the weight operand by 64 * FN tokens, the sum in blocks of 32.
-// Both operands of the forward pass have their sum contiguous: tile rows of 64 bytes, read as whole matrix operands by
-// ds_read_b128.  The input gradient's weights have it as the slow axis: tile rows of 512 bytes, through the transposing LDS
-// read.  Tiles go from global memory straight into LDS, four stages deep.  A direct load fills consecutive bytes, so rows
-// cannot be padded; instead the 16-byte unit u of a 64-byte row r lies at unit u ^ (r / 4 % 4), which keeps the 16 lanes of
-// an LDS access on different banks, and is paid for by the address a lane asks for, not by instructions.
+// A workgroup of eight wavefronts computes 256 rows of the weight operand by 64 * FN tokens, the sum in blocks of 64: 128
+// bytes of a row, a whole cache line.  (A load of 16 half lines takes the cache twice as long as one of 8 whole ones; blocks
+// of 32 took 1171 us instead of 1066 for 8192 tokens 4096 -> 10240.)  Tiles go from global memory straight into LDS: two
+// stages of weights, three of tokens, for FN = 4 all of a compute unit's 160 KB.  Both operands of the forward pass have
+// their sum contiguous: tile rows of 128 bytes, read as whole matrix operands by ds_read_b128.  The input gradient's weights
+// have it as the slow axis: tile rows of 512 bytes, through the transposing LDS read.  A direct load fills consecutive bytes,
+// so rows cannot be padded; instead the 16-byte unit u of a 128-byte row r lies at unit u ^ (r / 2 % 8), which keeps the
+// lanes of an LDS access on different banks and is paid for by the address a lane asks for, not by instructions.
 //
 // The two wavefronts of a SIMD alternate: while one multiplies a block (its matrix instructions back to back), the other
-// reads the fragments of its next block and issues its share of the direct loads; a workgroup barrier ends each phase.  The
-// second group of wavefronts enters the sequence one barrier late and leaves one out at the end.
-//   - The stage of block s is read in phases 2s (first group) and 2s + 1 (second); each read phase ends with the wait for
-//     its own reads, so behind the barrier of phase 2s + 1 nobody reads it.
-//   - The loads of block s + 3 are issued in phases 2s and 2s + 1, into the stage that block s - 1 left in phase 2s - 1.
-//   - At the end of its read phase a wavefront waits until only the loads of its two newest blocks are in flight: block
-//     s + 1 is then complete before phase 2s + 2 reads it.
-// Loads behind the last block repeat it, so that the counts are the same in every step; they fill stages nobody reads.
+// reads the fragments of its next block and issues direct loads; a workgroup barrier ends each phase.  The second group of
+// four wavefronts enters the sequence one barrier late and leaves one out at the end.
+//     phase           2s       2s + 1    2s + 2         (R reads, M multiplies)
+//     first group     R(s)     M(s)      R(s + 1)
+//     second group    M(s-1)   R(s)      M(s)
+// Block s is read in phases 2s and 2s + 1; every R ends with the wait for its own reads, so behind that barrier its stages
+// are free.  The first group loads the weights: those of block s + 1, in R(s), into the stage that block s - 1 left in phase
+// 2s - 1; it waits for them at the end of M(s).  The second group loads the tokens: those of block s + 2, in R(s), into the
+// stage that block s - 1 left; it waits for those of block s + 1, issued one R earlier, at the end of R(s).  Both are
+// complete before phase 2s + 2 reads them.
+//
+// A workgroup goes through several tiles, one per compute unit at a time, as one sequence of blocks: the loads run ahead into
+// the next tile, and a tile's results leave from registers in front of its group's next R, while the other group multiplies.
+// (A workgroup per tile started each with the latency of memory and ended with all of them storing at once: ViT-B's forward
+// pass took 122 us, 77 of it the sums.)  Loads behind the last tile's last block repeat it, so that the counts are the same in
+// every step; they fill stages nobody reads.
+//
 // Reads, waits and the barrier are asm because the compiler, which cannot tell the stages apart, would drain all loads in
 // front of every LDS read that it knows of.
 #include <algorithm>
@@ -28,31 +39,23 @@
 
 namespace dropit {
 
-// sixteen bytes that the lanes behind the end of a sum read
-__device__ __attribute__((aligned(16))) uint32_t gated_zeros[4];
-
 namespace {
 
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
-typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 
-constexpr int WIDE_THREADS = 512, WIDE_ROWS = 256, WIDE_K = 32, STAGES = 4, AHEAD = STAGES - 1;
-constexpr int W_BYTES = WIDE_ROWS * WIDE_K * 2, W_LOADS = W_BYTES / 1024 / 8;
+constexpr int WIDE_THREADS = 512, WIDE_ROWS = 256, WIDE_K = 64;
+constexpr int W_BYTES = WIDE_ROWS * WIDE_K * 2, W_STAGES = 2, X_STAGES = 3, X_AT = W_STAGES * W_BYTES;
+constexpr int W_LOADS = W_BYTES / 1024 / 4;            // of a wavefront of the first group and block
 constexpr int TOKEN_GROUP = 8;                         // token tiles that the workgroups of an XCD go through together
 
-template <bool FORWARD, int FN> struct Wide {
-    static constexpr int TOKENS = 64 * FN;
-    static constexpr int X_BYTES = TOKENS * WIDE_K * 2, X_LOADS = X_BYTES / 1024 / 8, LOADS = W_LOADS + X_LOADS;
-    static constexpr int STAGE_BYTES = W_BYTES + X_BYTES;
-    // the epilogue's staging areas, in the same bytes: COLS columns (and a pad that spreads rows over the banks) of 64 tokens,
-    // of h and both halves of pre or of dx, twice
-    static constexpr int COLS = FORWARD ? 128 : 256, PITCH = COLS + 8, PART = 64 * PITCH * 2, OUTS = FORWARD ? 3 : 1;
-    static constexpr int LDS_BYTES = STAGES * STAGE_BYTES > 2 * OUTS * PART ? STAGES * STAGE_BYTES : 2 * OUTS * PART;
-    static_assert(LDS_BYTES <= 160 * 1024, "LDS of one compute unit");
-    static_assert(X_BYTES % 8192 == 0, "the direct loads divide over eight wavefronts");
+template <int FN> struct Wide {
+    static constexpr int TOKENS = 64 * FN, X_BYTES = TOKENS * WIDE_K * 2, X_LOADS = X_BYTES / 1024 / 4;
+    static constexpr int LDS_BYTES = X_AT + X_STAGES * X_BYTES;
+    static_assert(FN >= 2 && FN <= 4 && LDS_BYTES <= 160 * 1024, "LDS of one compute unit");
 };
 
 template <int N> __device__ inline void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
@@ -85,68 +88,122 @@ template <bool FORWARD, int FN>
 __global__ void __launch_bounds__(WIDE_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2)))
 gated_wide_kernel(const WideArgs a)
 {
-    using C = Wide<FORWARD, FN>;
+    using C = Wide<FN>;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave >> 1, wn = wave & 1;           // 64 weight rows, 32 FN tokens
+    const bool late = wave >= 4;
 
-    // Workgroups are dealt to the 8 XCDs in turn: re-number so that those of one XCD are consecutive, and go through the
-    // weight tiles with TOKEN_GROUP token tiles at a time, whose operands then stay in that XCD's L2.
-    const int per_xcd = gridDim.x / 8;
-    const int v = int(blockIdx.x % 8) * per_xcd + int(blockIdx.x / 8);
-    if (v >= a.row_tiles * a.token_tiles) return;
-    const int group = v / (TOKEN_GROUP * a.row_tiles), within = v - group * TOKEN_GROUP * a.row_tiles;
-    const int size = min(TOKEN_GROUP, a.token_tiles - group * TOKEN_GROUP);
-    const int rt = within / size;
-    const int64_t t0 = int64_t(group * TOKEN_GROUP + within - rt * size) * C::TOKENS;
-    const int r0 = rt * (FORWARD ? WIDE_ROWS / 2 : WIDE_ROWS);      // first output column
+    // Workgroups are dealt to the 8 XCDs in turn.  An XCD's share of the tiles is consecutive, and its workgroups take them in
+    // turn; the order goes through the weight tiles with TOKEN_GROUP token tiles at a time, whose operands then stay in that
+    // XCD's L2.
+    const int tiles = a.row_tiles * a.token_tiles, per_xcd = (tiles + 7) / 8, stride = int(gridDim.x / 8);
+    const int v0 = int(blockIdx.x % 8) * per_xcd + int(blockIdx.x / 8);
+    const int v_end = min(int(blockIdx.x % 8 + 1) * per_xcd, tiles);
+    if (v0 >= v_end) return;
+    auto place = [&](int v, int &rt, int &tt) {
+        const int group = v / (TOKEN_GROUP * a.row_tiles), within = v - group * TOKEN_GROUP * a.row_tiles;
+        const int size = min(TOKEN_GROUP, a.token_tiles - group * TOKEN_GROUP);
+        rt = __builtin_amdgcn_readfirstlane(within / size);
+        tt = __builtin_amdgcn_readfirstlane(group * TOKEN_GROUP + within - rt * size);
+    };
     const int steps = (a.K + WIDE_K - 1) / WIDE_K;
-    const int tail = a.K - (steps - 1) * WIDE_K;       // of the last block: 8, 16, 24 or 32
+    const int tail = a.K - (steps - 1) * WIDE_K;       // of the last block: 8, 16, .. 64
 
-    // ---- global -> LDS: load q of a wavefront fills 1 KB of a tile, lane l the 16 bytes at l * 16
-    const char *src[C::LOADS];
-    bool in_tail[C::LOADS];
-    const int64_t w_step = FORWARD ? WIDE_K * 2 : int64_t(WIDE_K) * a.c_in * 2;
+    // ---- global -> LDS: load q of a wavefront fills 1 KB of a tile, lane l the 16 bytes at l * 16.  Through buffer descriptors:
+    // a lane gives 32 bits of address, the step is a scalar (64-bit addresses per lane cost the address unit 5 %), and what
+    // lies outside arrives as zeros: tokens and weight rows behind the last ones by their offset, which is a lane's own, and
+    // columns behind the last one and the last block's elements behind the end of the sum by an offset beyond every range.
+    // The descriptors' parts have to be scalars for the compiler too, or it puts a loop around every load.
+    constexpr uint32_t OUTSIDE = 0x80000000u;          // (gated_wide_takes: ranges are smaller)
+    constexpr int per_tile = FORWARD ? WIDE_ROWS / 2 : WIDE_ROWS;   // output columns
+    const int part = wave & 3;                         // of the group's tile
+    const uint32_t w_pitch = uint32_t(a.c_in) * 2u, x_pitch = uint32_t(a.K) * 2u;
+    // tile rows of 128 bytes: load q holds rows 8 (L part + q) + lane / 8 for L loads of a wavefront, whose units are turned by
+    // (row / 2) % 8, that is by lane / 16 and, for odd q (L is even), by 4 more.  Forward weights: row R of a wavefront's 64
+    // is gate row R for R < 32, then up rows of the same columns.  Tile rows of 512 bytes: load q holds k = 16 part + 2 q +
+    // lane / 32, turned by (k % 4) * 64 bytes.
+    const bool turned_tile = !FORWARD && !late;
+    const int first = late ? C::X_LOADS * part : W_LOADS * part;    // the wavefront's first load of the tile
+    const int unit = (lane & 7) ^ (lane >> 4);
+    uint32_t lane_off[2];                              // of even and odd q
+    int first_k[2];                                    // the sum's element in a block that a lane's even / odd loads start at
+    uint32_t q_step;                                   // from a load to the next but one
+    uint32_t column[2] = {0, 0};                       // (turned tile) byte of the row, within the tile's columns
+    if (turned_tile) {
 #pragma unroll
-    for (int q = 0; q < W_LOADS; ++q) {
-        const int o = (wave * W_LOADS + q) * 1024 + lane * 16;
-        if constexpr (FORWARD) {
-            const int R = o / 64, unit = (o / 16 & 3) ^ (R >> 2 & 3);
-            // rows R of a wavefront's 64: 32 gate rows, then the up rows of the same columns
-            const int n = min(r0 + (R >> 6) * 32 + (R & 31), a.hidden - 1);
-            src[q] = static_cast<const char *>(a.w) + ((R & 32 ? int64_t(a.hidden) : 0) + n) * a.c_in * 2 + unit * 16;
-            in_tail[q] = unit * 8 < tail;
-        } else {
-            const int k = o / 512, c = min(r0 + ((o & 511) ^ ((k & 3) << 6)) / 2, a.c_in - 8);
-            src[q] = static_cast<const char *>(a.w) + (int64_t(k) * a.c_in + c) * 2;
-            in_tail[q] = k < tail;
+        for (int o = 0; o < 2; ++o) {
+            first_k[o] = 16 * part + 2 * o + (lane >> 5);
+            column[o] = uint32_t(((lane & 31) * 16) ^ ((first_k[o] & 3) << 6));
+            lane_off[o] = uint32_t(first_k[o]) * w_pitch + column[o];
         }
-    }
+        q_step = 4u * w_pitch;
+    } else {
+        const uint32_t pitch = late ? x_pitch : w_pitch;
+        const uint32_t row = uint32_t((late ? 8 * first : 32 * part) + (lane >> 3));
 #pragma unroll
-    for (int q = 0; q < C::X_LOADS; ++q) {
-        const int o = (wave * C::X_LOADS + q) * 1024 + lane * 16;
-        const int r = o / 64, unit = (o / 16 & 3) ^ (r >> 2 & 3);
-        src[W_LOADS + q] = static_cast<const char *>(a.x) + min<int64_t>(t0 + r, a.tokens - 1) * a.K * 2 + unit * 16;
-        in_tail[W_LOADS + q] = unit * 8 < tail;
+        for (int o = 0; o < 2; ++o) {
+            first_k[o] = (unit ^ (4 * o)) * 8;
+            lane_off[o] = (row + 8u * o) * pitch + uint32_t(first_k[o]) * 2u;
+        }
+        q_step = 16u * pitch;
     }
-    auto issue_load = [&](auto q_, int stage, int s) {
+    const uint32_t up_step = FORWARD && !late ? uint32_t(a.hidden - 32) * w_pitch : 0u;     // loads 4 .. 7 of forward weights
+    const int s_step = turned_tile ? WIDE_K * int(w_pitch) : WIDE_K * 2;
+    // the loads' own place in the sequence of blocks, and their tile's descriptor
+    int lv = v0, ls = 0;
+    const char *l_base;
+    int l_range;
+    uint32_t l_outside[2];                             // OUTSIDE for lanes behind the last column
+    auto load_tile = [&]() {
+        int rt, tt;
+        place(lv, rt, tt);
+        l_outside[0] = l_outside[1] = 0u;
+        if (late) {
+            l_base = static_cast<const char *>(a.x) + int64_t(tt) * C::TOKENS * a.K * 2;
+            l_range = min(int(a.tokens) - tt * C::TOKENS, C::TOKENS) * a.K * 2;
+        } else if constexpr (FORWARD) {
+            l_base = static_cast<const char *>(a.w) + int64_t(rt) * per_tile * a.c_in * 2;
+            l_range = (2 * a.hidden - rt * per_tile) * a.c_in * 2;
+        } else {
+            l_base = static_cast<const char *>(a.w) + int64_t(rt) * per_tile * 2;
+            l_range = 2 * a.hidden * a.c_in * 2 - rt * per_tile * 2;
+#pragma unroll
+            for (int o = 0; o < 2; ++o) l_outside[o] = uint32_t(rt * per_tile) * 2u + column[o] < w_pitch ? 0u : OUTSIDE;
+        }
+    };
+    load_tile();
+    auto advance = [&]() {
+        if (ls + 1 < steps) {
+            ++ls;
+        } else if (lv + stride < v_end) {
+            lv += stride;
+            ls = 0;
+            load_tile();
+        }
+    };
+    auto issue_load = [&](auto q_, char *tile) {
         constexpr int q = decltype(q_)::value;
-        const char *p = src[q] + s * (q < W_LOADS ? w_step : int64_t(WIDE_K * 2));
-        if (s == steps - 1) p = in_tail[q] ? p : reinterpret_cast<const char *>(gated_zeros);
-        char *to = lds + stage * C::STAGE_BYTES + (q < W_LOADS ? (wave * W_LOADS + q) * 1024 : W_BYTES + (wave * C::X_LOADS + q - W_LOADS) * 1024);
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)p,
-                                         (__attribute__((address_space(3))) void *)to, 16, 0, 0);
+        if (q >= C::X_LOADS && late) return;
+        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(l_base), 0, l_range, 0x00020000);
+        uint32_t at = lane_off[q & 1] + (q >> 1) * q_step + (q >= 4 ? up_step : 0u);
+        if constexpr (!FORWARD) at |= l_outside[q & 1];
+        const int k = first_k[q & 1] + (turned_tile ? (q >> 1) * 4 : 0);
+        if (ls == steps - 1) at = k < tail ? at : OUTSIDE;
+        const int scalar = ls * s_step;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void *)(tile + (first + q) * 1024), 16, int(at),
+                                                 scalar, 0, 0);
     };
 
     // ---- LDS -> fragments: operand lane l takes row l % 32 and the sum's elements 8 (l / 32) .. + 7 of 16
     const uint32_t base = uint32_t(size_t((__attribute__((address_space(3))) void *)lds));
     const int row = lane & 31, half = lane >> 5;
-    const uint32_t unit0 = uint32_t(half ^ (row >> 2 & 3)) * 16;    // (32 rows further on the same: 32 / 4 is a multiple of 4)
-    const uint32_t x_at = W_BYTES + uint32_t(wn * 32 * FN + row) * 64 + unit0;
+    const uint32_t unit0 = uint32_t(half ^ (row >> 1 & 7)) * 16;    // (32 rows further on the same: 32 / 2 is a multiple of 8)
+    const uint32_t x_at = X_AT + uint32_t(wn * 32 * FN + row) * 128 + unit0;
     uint32_t w_at[2];
     if constexpr (FORWARD) {
-        w_at[0] = uint32_t(wm * 64 + row) * 64 + unit0;
+        w_at[0] = uint32_t(wm * 64 + row) * 128 + unit0;
         w_at[1] = 0;
     } else {
         const int g = lane >> 4, p16 = lane & 15, krow = (g >> 1) * 8 + (p16 >> 2);
@@ -154,160 +211,173 @@ gated_wide_kernel(const WideArgs a)
         for (int i = 0; i < 2; ++i)
             w_at[i] = uint32_t(krow * 512 + (((wm * 64 + i * 32 + (g & 1) * 16 + (p16 & 3) * 4) * 2) ^ ((p16 >> 2) << 6)));
     }
-    u32x4 fw[2][2], fx[2][FN];                         // of both 16-deep halves of a block
-    u32x2 ft[2][2][2];                                 // (transposing reads bring half an operand each)
-    auto read_half = [&](auto kk_, uint32_t stage_base) {
+    constexpr int KK = WIDE_K / 16;                    // depths of one matrix instruction
+    u32x4 fw[KK][2], fx[KK][FN];
+    u32x2 ft[KK][2][2];                                // (transposing reads bring half an operand each)
+    auto read_depth = [&](auto kk_, uint32_t w_base, uint32_t x_base) {
         constexpr int kk = decltype(kk_)::value;
         if constexpr (FORWARD) {
-            const uint32_t at = stage_base + (w_at[0] ^ (kk * 32));
+            const uint32_t at = w_base + (w_at[0] ^ (kk * 32));
             fw[kk][0] = read16<0>(at);
-            fw[kk][1] = read16<32 * 64>(at);
+            fw[kk][1] = read16<32 * 128>(at);
         } else {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                ft[kk][i][0] = read_turned<kk * 16 * 512>(stage_base + w_at[i]);
-                ft[kk][i][1] = read_turned<(kk * 16 + 4) * 512>(stage_base + w_at[i]);
+                ft[kk][i][0] = read_turned<kk * 16 * 512>(w_base + w_at[i]);
+                ft[kk][i][1] = read_turned<(kk * 16 + 4) * 512>(w_base + w_at[i]);
             }
         }
-        const uint32_t at = stage_base + (x_at ^ (kk * 32));
-        static_for<0, FN>([&](auto j_) { fx[kk][decltype(j_)::value] = read16<decltype(j_)::value * 32 * 64>(at); });
+        const uint32_t at = x_base + (x_at ^ (kk * 32));
+        static_for<0, FN>([&](auto j_) { fx[kk][decltype(j_)::value] = read16<decltype(j_)::value * 32 * 128>(at); });
     };
 
-    f32x16 acc[2][FN];
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < FN; ++j)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
-
-    const bool late = wave >= 4;
-#pragma unroll
-    for (int d = 0; d < AHEAD; ++d) static_for<0, C::LOADS>([&](auto q_) { issue_load(q_, d, min(d, steps - 1)); });
-    wait_loads<(AHEAD - 1) * C::LOADS>();
+    // the first block's weights, the first two blocks' tokens
+    static_for<0, W_LOADS>([&](auto q_) { issue_load(q_, lds + (late ? X_AT : 0)); });
+    if (late) {
+        advance();
+        static_for<0, W_LOADS>([&](auto q_) { issue_load(q_, lds + X_AT + C::X_BYTES); });
+        wait_loads<C::X_LOADS>();
+    } else {
+        wait_loads<0>();
+    }
     workgroup_barrier();
     if (late) workgroup_barrier();
-    int stage = 0, fill = AHEAD;
-    for (int s = 0; s < steps; ++s) {
-        const uint32_t stage_base = base + stage * C::STAGE_BYTES;
-        const int next = min(s + AHEAD, steps - 1);
-        static_for<0, 2>([&](auto kk_) {
-            constexpr int kk = decltype(kk_)::value;
-            read_half(kk_, stage_base);
-            static_for<kk * C::LOADS / 2, (kk + 1) * C::LOADS / 2>([&](auto q_) { issue_load(q_, fill, next); });
-        });
-        wait_lds();
-        wait_loads<(AHEAD - 1) * C::LOADS>();
-        __builtin_amdgcn_sched_barrier(0);
-        workgroup_barrier();
-        __builtin_amdgcn_sched_barrier(0);
-        static_for<0, 2>([&](auto kk_) {
-            constexpr int kk = decltype(kk_)::value;
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {              // (nothing may move a fragment before the wait above)
-                if constexpr (FORWARD) {
-                    asm volatile("" : "+v"(fw[kk][i]));
-                } else {
-                    asm volatile("" : "+v"(ft[kk][i][0]), "+v"(ft[kk][i][1]));
-                    fw[kk][i] = __builtin_shufflevector(ft[kk][i][0], ft[kk][i][1], 0, 1, 2, 3);
-                }
-            }
-#pragma unroll
-            for (int j = 0; j < FN; ++j) asm volatile("" : "+v"(fx[kk][j]));
-            static_for<0, 2 * FN>([&](auto m_) {
-                constexpr int m = decltype(m_)::value, i = m / FN, j = m % FN;
-                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fw[kk][i]),
-                                                                    __builtin_bit_cast(bf16x8, fx[kk][j]), acc[i][j], 0, 0, 0);
-                __builtin_amdgcn_sched_barrier(0);
-            });
-        });
-        if (!(late && s + 1 == steps)) workgroup_barrier();
-        __builtin_amdgcn_sched_barrier(0);
-        stage = stage + 1 == STAGES ? 0 : stage + 1;
-        fill = fill + 1 == STAGES ? 0 : fill + 1;
-    }
-    wait_loads<0>();                                   // nothing may still be writing LDS
-    __syncthreads();
-
-    // ---- out, 64 tokens at a time (32 of each half of the tile) by way of LDS, in rows of 16-byte units.  Lane l holds token
-    // l % 32 and, in register 4 q + e, row 8 q + 4 (l / 32) + e of each 32 x 32 block.
-    constexpr int COLS = C::COLS, PITCH = C::PITCH, PART = C::PART, OUTS = C::OUTS;
-    const int width = FORWARD ? a.hidden : a.c_in;
-    float bias[2][16];
-    if constexpr (FORWARD) {
+    int w_stage = 0, x_stage = 0;
+    for (int v = v0; v < v_end; v += stride) {
+        f32x16 acc[2][FN];
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
+            for (int j = 0; j < FN; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int n = min(r0 + wm * 32 + q * 8 + half * 4 + e, a.hidden - 1) + i * a.hidden;
-                    bias[i][q * 4 + e] = a.bias != nullptr ? __uint_as_float(uint32_t(static_cast<const uint16_t *>(a.bias)[n]) << 16) : 0.f;
+                for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+        for (int s = 0; s < steps; ++s) {
+            const uint32_t w_base = base + w_stage * W_BYTES, x_base = base + x_stage * C::X_BYTES;
+            w_stage ^= 1;                              // the next block's weights
+            const int x_fill = x_stage == 0 ? X_STAGES - 1 : x_stage - 1;       // the next but one's tokens
+            x_stage = x_stage == X_STAGES - 1 ? 0 : x_stage + 1;
+            char *const fill = lds + (late ? X_AT + x_fill * C::X_BYTES : w_stage * W_BYTES);
+            advance();
+            static_for<0, KK>([&](auto kk_) {
+                constexpr int kk = decltype(kk_)::value;
+                read_depth(kk_, w_base, x_base);
+                static_for<kk * W_LOADS / KK, (kk + 1) * W_LOADS / KK>([&](auto q_) { issue_load(q_, fill); });
+            });
+            wait_lds();
+            if (late) wait_loads<C::X_LOADS>();
+            __builtin_amdgcn_sched_barrier(0);
+            workgroup_barrier();
+            __builtin_amdgcn_sched_barrier(0);
+            static_for<0, KK>([&](auto kk_) {
+                constexpr int kk = decltype(kk_)::value;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {          // (nothing may move a fragment before the wait above)
+                    if constexpr (FORWARD) {
+                        asm volatile("" : "+v"(fw[kk][i]));
+                    } else {
+                        asm volatile("" : "+v"(ft[kk][i][0]), "+v"(ft[kk][i][1]));
+                        fw[kk][i] = __builtin_shufflevector(ft[kk][i][0], ft[kk][i][1], 0, 1, 2, 3);
+                    }
                 }
-    }
-    auto put = [&](char *area, int col, float v0, float v1, float v2, float v3) {
-        *reinterpret_cast<bf16x4 *>(area + ((wn * 32 + row) * PITCH + col) * 2) =
-            bf16x4{static_cast<__bf16>(v0), static_cast<__bf16>(v1), static_cast<__bf16>(v2), static_cast<__bf16>(v3)};
-    };
-    auto copy_out = [&](const char *area, void *out, int64_t pitch, int64_t at, int j) {
-        constexpr int UNITS = COLS / 8;
 #pragma unroll
-        for (int r = 0; r < 64 * UNITS / WIDE_THREADS; ++r) {
-            const int u = r * WIDE_THREADS + int(threadIdx.x), token = u / UNITS, c = u % UNITS * 8;
-            const int64_t t = t0 + (token >> 5) * 32 * FN + j * 32 + (token & 31);
-            const int n = r0 + c;
-            if (t >= a.tokens || n >= width) continue;
-            uint16_t *to = static_cast<uint16_t *>(out) + t * pitch + at + n;
-            const u32x4 w = *reinterpret_cast<const u32x4 *>(area + (token * PITCH + c) * 2);
-            if (width % 8 == 0) {                      // (then every row starts on 16 bytes)
-                *reinterpret_cast<u32x4 *>(to) = w;
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (n + e < width) to[e] = uint16_t(w[e >> 1] >> (16 * (e & 1)));
-            }
+                for (int j = 0; j < FN; ++j) asm volatile("" : "+v"(fx[kk][j]));
+                static_for<0, 2 * FN>([&](auto m_) {
+                    constexpr int m = decltype(m_)::value, i = m / FN, j = m % FN;
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fw[kk][i]),
+                                                                        __builtin_bit_cast(bf16x8, fx[kk][j]), acc[i][j], 0, 0, 0);
+                    __builtin_amdgcn_sched_barrier(0);
+                });
+            });
+            if (!late) wait_loads<0>();
+            __builtin_amdgcn_sched_barrier(0);
+            if (!(late && s + 1 == steps && v + stride >= v_end)) workgroup_barrier();
+            __builtin_amdgcn_sched_barrier(0);
         }
-    };
-    static_for<0, FN>([&](auto j_) {
-        constexpr int j = decltype(j_)::value;
-        char *area = lds + (j & 1) * OUTS * PART;      // (the pass before reads the other one)
+
+        // ---- out: lane l holds token l % 32 and, in register 4 q + e, row 8 q + 4 (l / 32) + e of each 32 x 32 block.  The
+        // halves of the wavefront trade their columns of every other eight, so that a lane stores 16 bytes of a row and two
+        // lanes 32.
+        int rt, tt;
+        place(v, rt, tt);
+        const int64_t t0 = int64_t(tt) * C::TOKENS;
+        const int width = FORWARD ? a.hidden : a.c_in;
+        const int n0 = rt * per_tile + wm * (FORWARD ? 32 : 64);
+        auto store_block = [&](const float (&x)[16], void *out, int64_t pitch, int64_t at, int n, int j) {
+            const int64_t t = t0 + wn * 32 * FN + j * 32 + row;
+            uint16_t *to = static_cast<uint16_t *>(out) + t * pitch + at;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            if constexpr (FORWARD) {
-                float g[4], u[4], h[4];
+            for (int q = 0; q < 4; q += 2) {
+                uint32_t d[2][2];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    g[e] = acc[0][j][q * 4 + e] + bias[0][q * 4 + e];
-                    u[e] = acc[1][j][q * 4 + e] + bias[1][q * 4 + e];
-                    h[e] = activation<true>(g[e], a.act) * u[e];
+                for (int p = 0; p < 2; ++p)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const bf16x2 pair = {static_cast<__bf16>(x[(q + p) * 4 + 2 * e]), static_cast<__bf16>(x[(q + p) * 4 + 2 * e + 1])};
+                        d[p][e] = __builtin_bit_cast(uint32_t, pair);
+                    }
+                u32x4 w;
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const auto r = __builtin_amdgcn_permlane32_swap(d[0][e], d[1][e], false, false);
+                    w[e] = r[0];
+                    w[2 + e] = r[1];
                 }
-                const int col = wm * 32 + q * 8 + half * 4;
-                put(area, col, h[0], h[1], h[2], h[3]);
-                if (a.pre != nullptr) {
-                    put(area + PART, col, g[0], g[1], g[2], g[3]);
-                    put(area + 2 * PART, col, u[0], u[1], u[2], u[3]);
-                }
-            } else {
+                const int c = n + (q + half) * 8;
+                if (t >= a.tokens || c >= width) continue;
+                if (width % 8 == 0) {                  // (then every row starts on 16 bytes)
+                    *reinterpret_cast<u32x4 *>(to + c) = w;
+                } else {
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
-                    put(area, wm * 64 + i * 32 + q * 8 + half * 4, acc[i][j][q * 4], acc[i][j][q * 4 + 1], acc[i][j][q * 4 + 2], acc[i][j][q * 4 + 3]);
+                    for (int e = 0; e < 8; ++e)
+                        if (c + e < width) to[c + e] = uint16_t(w[e >> 1] >> (16 * (e & 1)));
+                }
             }
-        }
-        __syncthreads();
-        copy_out(area, a.out, width, 0, j);
+        };
         if constexpr (FORWARD) {
-            if (a.pre != nullptr) {
-                copy_out(area + PART, a.pre, 2 * int64_t(width), 0, j);
-                copy_out(area + 2 * PART, a.pre, 2 * int64_t(width), width, j);
+            float bias[2][16];
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int n = min(n0 + (r >> 2) * 8 + half * 4 + (r & 3), a.hidden - 1) + i * a.hidden;
+                    bias[i][r] = a.bias != nullptr ? __uint_as_float(uint32_t(static_cast<const uint16_t *>(a.bias)[n]) << 16) : 0.f;
+                }
+#pragma unroll
+            for (int j = 0; j < FN; ++j) {
+                float x[16], u[16];
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    x[r] = acc[0][j][r] + bias[0][r];
+                    u[r] = acc[1][j][r] + bias[1][r];
+                }
+                if (a.pre != nullptr) {
+                    store_block(x, a.pre, 2 * int64_t(width), 0, n0, j);
+                    store_block(u, a.pre, 2 * int64_t(width), width, n0, j);
+                }
+                activations<true>(x, a.act);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) x[r] *= u[r];
+                store_block(x, a.out, width, 0, n0, j);
             }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < FN; ++j) {
+                    float x[16];
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) x[r] = acc[i][j][r];
+                    store_block(x, a.out, width, 0, n0 + i * 32, j);
+                }
         }
-    });
+    }
+    wait_loads<0>();                                   // nothing may still be writing LDS
 }
 
 template <bool FORWARD, int FN>
 dropit_status launch(WideArgs a, hipStream_t stream)
 {
-    using C = Wide<FORWARD, FN>;
+    using C = Wide<FN>;
     constexpr int per_tile = FORWARD ? WIDE_ROWS / 2 : WIDE_ROWS;
     static std::atomic<uint64_t> done{0};
     if (!once_per_device(done, [] {
@@ -318,7 +388,8 @@ dropit_status launch(WideArgs a, hipStream_t stream)
     a.row_tiles = ((FORWARD ? a.hidden : a.c_in) + per_tile - 1) / per_tile;
     a.token_tiles = int((a.tokens + C::TOKENS - 1) / C::TOKENS);
     const int64_t tiles = int64_t(a.row_tiles) * a.token_tiles;
-    gated_wide_kernel<FORWARD, FN><<<static_cast<uint32_t>((tiles + 7) / 8 * 8), WIDE_THREADS, C::LDS_BYTES, stream>>>(a);
+    const uint32_t grid = static_cast<uint32_t>(std::min<int64_t>((tiles + 7) / 8 * 8, 256));       // one per compute unit
+    gated_wide_kernel<FORWARD, FN><<<grid, WIDE_THREADS, C::LDS_BYTES, stream>>>(a);
     return launch_status();
 }
 
@@ -326,12 +397,36 @@ dropit_status launch(WideArgs a, hipStream_t stream)
 
 bool gated_wide_takes(int64_t tokens, int c_in, int hidden, bool forward)
 {
-    return tokens >= 128 && c_in % 8 == 0 && (forward || hidden % 4 == 0);
+    // rows in 16-byte units; the weights, and 256 tokens, below 2^31 bytes
+    return tokens >= 128 && c_in % 8 == 0 && (forward || hidden % 4 == 0) && 4 * int64_t(hidden) * c_in < int64_t(1) << 31 &&
+           std::max(c_in, 2 * hidden) < 1 << 22;
 }
 
 dropit_status launch_gated_wide(const WideArgs &a, bool forward, hipStream_t stream)
 {
-    return forward ? launch<true, 4>(a, stream) : launch<false, 4>(a, stream);
+    // How many tokens to a tile: what the compute unit with the most tiles takes, a block of the sum and a tile's start and
+    // end at what they were measured to cost (us; whole chip busy: blocks of 8192 tokens 4096 -> 10240 both ways, ends of
+    // ViT-B's and DeiT-S's forward passes).  Fewer tokens cost more LDS reads per matrix instruction: 64 of them as much as 128
+    // per block, so there is no such tile.  us for 256, 192 and 128 tokens: 12608 tokens 768 -> 2048 forward 109, 105, 123,
+    // backward 81, 74, 108; 25216 tokens 384 -> 1024 75, 73, 77 and 50, 67, 59; 2048 tokens 2048 -> 5632 93, 84, 93 and
+    // 169, 137, 128; 8192 tokens 4096 -> 10240 1004, 1095, 1365.
+    constexpr double block_us[3] = {1.07, 1.22, 1.57}, end_us[3] = {4.7, 6.3, 8.0};
+    const int64_t rows = forward ? (a.hidden + WIDE_ROWS / 2 - 1) / (WIDE_ROWS / 2) : (a.c_in + WIDE_ROWS - 1) / WIDE_ROWS;
+    const int64_t blocks = (a.K + WIDE_K - 1) / WIDE_K;
+    int best = 0;
+    double best_us = 0.0;
+    for (int f = 0; f < 3; ++f) {
+        const int64_t tiles = rows * ((a.tokens + 64 * (f + 2) - 1) / (64 * (f + 2)));
+        const int64_t rounds = ((tiles + 7) / 8 + 31) / 32;         // of 32 compute units on each of 8 XCDs
+        const double us = double(rounds) * (double(blocks) * block_us[f] + end_us[f]);
+        if (f == 0 || us <= best_us) {
+            best = f;
+            best_us = us;
+        }
+    }
+    if (best == 2) return forward ? launch<true, 4>(a, stream) : launch<false, 4>(a, stream);
+    if (best == 1) return forward ? launch<true, 3>(a, stream) : launch<false, 3>(a, stream);
+    return forward ? launch<true, 2>(a, stream) : launch<false, 2>(a, stream);
 }
 
 }  // namespace dropit
