@@ -255,6 +255,13 @@ int gen_splits(int64_t tokens, int rows, int per_tile, int64_t K)
 }
 
 template <bool BF16, bool FORWARD>
+void launch_finish(const GenArgs &a, hipStream_t stream)
+{
+    const int64_t blocks = (a.tokens * (FORWARD ? a.hidden : a.c_in) + 255) / 256;
+    gated_finish_kernel<BF16, FORWARD><<<static_cast<uint32_t>(std::min<int64_t>(blocks, 1 << 16)), 256, 0, stream>>>(a);
+}
+
+template <bool BF16, bool FORWARD>
 dropit_status launch_generic(GenArgs a, hipStream_t stream)
 {
     constexpr int per_tile = FORWARD ? GEN_ROWS / 2 : GEN_ROWS;
@@ -268,10 +275,30 @@ dropit_status launch_generic(GenArgs a, hipStream_t stream)
     const bool vec = a.c_in % Elem<BF16>::PER16 == 0 && a.K % Elem<BF16>::PER16 == 0;
     if (vec) gated_product_kernel<BF16, FORWARD, true><<<grid, GEN_THREADS, 0, stream>>>(a);
     else gated_product_kernel<BF16, FORWARD, false><<<grid, GEN_THREADS, 0, stream>>>(a);
-    if (a.splits > 1) {
-        const int64_t blocks = (a.tokens * rows + 255) / 256;
-        gated_finish_kernel<BF16, FORWARD><<<static_cast<uint32_t>(std::min<int64_t>(blocks, 1 << 16)), 256, 0, stream>>>(a);
-    }
+    if (a.splits > 1) launch_finish<BF16, FORWARD>(a, stream);
+    return launch_status();
+}
+
+// bf16 on wide tiles
+template <bool FORWARD>
+dropit_status launch_wide(GenArgs a, const WidePlan &plan, hipStream_t stream)
+{
+    WideArgs w{};
+    w.w = a.w;
+    w.x = a.x;
+    w.tokens = a.tokens;
+    w.hidden = a.hidden;
+    w.c_in = a.c_in;
+    w.K = a.K;
+    w.act = a.act;
+    w.bias = a.bias;
+    w.out = a.out;
+    w.pre = a.pre;
+    w.partial = a.partial;
+    w.splits = a.splits = plan.splits;
+    const dropit_status st = launch_gated_wide(w, plan, FORWARD, stream);
+    if (st != DROPIT_OK || plan.splits == 1) return st;
+    launch_finish<true, FORWARD>(a, stream);
     return launch_status();
 }
 
@@ -382,22 +409,6 @@ gated_bias_kernel(const float *__restrict__ partial, int64_t blocks, int64_t wid
 
 int64_t row_blocks(int64_t tokens) { return (tokens + SLOPE_ROWS - 1) / SLOPE_ROWS; }
 
-WideArgs wide_args(const GenArgs &g)
-{
-    WideArgs a{};
-    a.w = g.w;
-    a.x = g.x;
-    a.tokens = g.tokens;
-    a.hidden = g.hidden;
-    a.c_in = g.c_in;
-    a.K = g.K;
-    a.act = g.act;
-    a.bias = g.bias;
-    a.out = g.out;
-    a.pre = g.pre;
-    return a;
-}
-
 bool valid_sizes(int64_t tokens, int64_t c_in, int64_t hidden, dropit_dtype dt)
 {
     if (tokens < 0 || tokens > INT32_MAX || c_in < 1 || c_in > 1 << 28 || hidden < 1 || hidden > 1 << 27) return false;
@@ -409,15 +420,17 @@ bool valid_sizes(int64_t tokens, int64_t c_in, int64_t hidden, dropit_dtype dt)
 
 size_t forward_bytes(int64_t tokens, int64_t c_in, int64_t hidden, dropit_dtype dt)
 {
-    if (dt == DROPIT_BF16 && gated_wide_takes(tokens, int(c_in), int(hidden), true)) return 0;
-    const int splits = tokens == 0 ? 1 : gen_splits(tokens, int(hidden), GEN_ROWS / 2, c_in);
+    if (tokens == 0 || gated_tokens_takes(tokens, c_in, hidden, dt)) return 0;
+    const WidePlan plan = gated_wide_plan(tokens, c_in, hidden, true);
+    const int splits = dt == DROPIT_BF16 && plan.takes ? plan.splits : gen_splits(tokens, int(hidden), GEN_ROWS / 2, c_in);
     return splits == 1 ? 0 : size_t(splits) * tokens * 2 * hidden * sizeof(float);
 }
 
 size_t dx_bytes(int64_t tokens, int64_t c_in, int64_t hidden, dropit_dtype dt)
 {
-    if (dt == DROPIT_BF16 && gated_wide_takes(tokens, int(c_in), int(hidden), false)) return 0;
-    const int splits = tokens == 0 ? 1 : gen_splits(tokens, int(c_in), GEN_ROWS, 2 * hidden);
+    if (tokens == 0) return 0;
+    const WidePlan plan = gated_wide_plan(tokens, c_in, hidden, false);
+    const int splits = dt == DROPIT_BF16 && plan.takes ? plan.splits : gen_splits(tokens, int(c_in), GEN_ROWS, 2 * hidden);
     return splits == 1 ? 0 : size_t(splits) * tokens * c_in * sizeof(float);
 }
 
@@ -456,7 +469,9 @@ extern "C" dropit_status dropit_gated_forward(const void *x, int64_t tokens, int
     a.out = h;
     a.pre = pre;
     a.partial = static_cast<float *>(workspace);
-    if (dt == DROPIT_BF16 && gated_wide_takes(tokens, a.c_in, a.hidden, true)) return launch_gated_wide(wide_args(a), true, stream);
+    if (gated_tokens_takes(tokens, c_in, hidden, dt)) return launch_gated_tokens(x, tokens, a.c_in, dt, w, bias, a.hidden, act, h, pre, stream);
+    const WidePlan plan = gated_wide_plan(tokens, c_in, hidden, true);
+    if (dt == DROPIT_BF16 && plan.takes) return launch_wide<true>(a, plan, stream);
     return dt == DROPIT_BF16 ? launch_generic<true, true>(a, stream) : launch_generic<false, true>(a, stream);
 }
 
@@ -520,6 +535,7 @@ extern "C" dropit_status dropit_gated_backward(const void *dh, const void *pre, 
     a.act = act;
     a.out = dx;
     a.partial = static_cast<float *>(workspace);
-    if (bf16 && gated_wide_takes(tokens, a.c_in, a.hidden, false)) return launch_gated_wide(wide_args(a), false, stream);
+    const WidePlan plan = gated_wide_plan(tokens, c_in, hidden, false);
+    if (bf16 && plan.takes) return launch_wide<false>(a, plan, stream);
     return bf16 ? launch_generic<true, false>(a, stream) : launch_generic<false, false>(a, stream);
 }

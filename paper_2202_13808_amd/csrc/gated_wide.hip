@@ -45,6 +45,7 @@ typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 
 constexpr int WIDE_THREADS = 512, WIDE_ROWS = 256, WIDE_K = 64;
@@ -84,7 +85,8 @@ template <int I, int N, typename F> __device__ inline void static_for(F &&f)
     }
 }
 
-template <bool FORWARD, int FN>
+// SLICED: the sum in a.splits slices, partial sums out
+template <bool FORWARD, int FN, bool SLICED>
 __global__ void __launch_bounds__(WIDE_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2)))
 gated_wide_kernel(const WideArgs a)
 {
@@ -98,11 +100,13 @@ gated_wide_kernel(const WideArgs a)
     // Workgroups are dealt to the 8 XCDs in turn.  An XCD's share of the tiles is consecutive, and its workgroups take them in
     // turn; the order goes through the weight tiles with TOKEN_GROUP token tiles at a time, whose operands then stay in that
     // XCD's L2.
-    const int tiles = a.row_tiles * a.token_tiles, per_xcd = (tiles + 7) / 8, stride = int(gridDim.x / 8);
+    const int slice_tiles = a.row_tiles * a.token_tiles, tiles = SLICED ? slice_tiles * a.splits : slice_tiles, per_xcd = (tiles + 7) / 8, stride = int(gridDim.x / 8);
     const int v0 = int(blockIdx.x % 8) * per_xcd + int(blockIdx.x / 8);
     const int v_end = min(int(blockIdx.x % 8 + 1) * per_xcd, tiles);
     if (v0 >= v_end) return;
-    auto place = [&](int v, int &rt, int &tt) {
+    auto place = [&](int v, int &rt, int &tt, int &slice) {
+        slice = SLICED ? __builtin_amdgcn_readfirstlane(v / slice_tiles) : 0;
+        v -= slice * slice_tiles;
         const int group = v / (TOKEN_GROUP * a.row_tiles), within = v - group * TOKEN_GROUP * a.row_tiles;
         const int size = min(TOKEN_GROUP, a.token_tiles - group * TOKEN_GROUP);
         rt = __builtin_amdgcn_readfirstlane(within / size);
@@ -110,6 +114,7 @@ gated_wide_kernel(const WideArgs a)
     };
     const int steps = (a.K + WIDE_K - 1) / WIDE_K;
     const int tail = a.K - (steps - 1) * WIDE_K;       // of the last block: 8, 16, .. 64
+    auto slice_begin = [&](int slice) { return SLICED ? __builtin_amdgcn_readfirstlane(int(int64_t(steps) * slice / a.splits)) : slice * steps; };
 
     // ---- global -> LDS: load q of a wavefront fills 1 KB of a tile, lane l the 16 bytes at l * 16.  Through buffer descriptors:
     // a lane gives 32 bits of address, the step is a scalar (64-bit addresses per lane cost the address unit 5 %), and what
@@ -152,13 +157,15 @@ gated_wide_kernel(const WideArgs a)
     const uint32_t up_step = FORWARD && !late ? uint32_t(a.hidden - 32) * w_pitch : 0u;     // loads 4 .. 7 of forward weights
     const int s_step = turned_tile ? WIDE_K * int(w_pitch) : WIDE_K * 2;
     // the loads' own place in the sequence of blocks, and their tile's descriptor
-    int lv = v0, ls = 0;
+    int lv = v0, ls, l_end;
     const char *l_base;
     int l_range;
     uint32_t l_outside[2];                             // OUTSIDE for lanes behind the last column
     auto load_tile = [&]() {
-        int rt, tt;
-        place(lv, rt, tt);
+        int rt, tt, slice;
+        place(lv, rt, tt, slice);
+        ls = slice_begin(slice);
+        l_end = slice_begin(slice + 1);
         l_outside[0] = l_outside[1] = 0u;
         if (late) {
             l_base = static_cast<const char *>(a.x) + int64_t(tt) * C::TOKENS * a.K * 2;
@@ -175,11 +182,10 @@ gated_wide_kernel(const WideArgs a)
     };
     load_tile();
     auto advance = [&]() {
-        if (ls + 1 < steps) {
+        if (ls + 1 < l_end) {
             ++ls;
         } else if (lv + stride < v_end) {
             lv += stride;
-            ls = 0;
             load_tile();
         }
     };
@@ -244,6 +250,11 @@ gated_wide_kernel(const WideArgs a)
     if (late) workgroup_barrier();
     int w_stage = 0, x_stage = 0;
     for (int v = v0; v < v_end; v += stride) {
+        int blocks = steps;
+        if constexpr (SLICED) {
+            const int slice = __builtin_amdgcn_readfirstlane(v / slice_tiles);
+            blocks = slice_begin(slice + 1) - slice_begin(slice);
+        }
         f32x16 acc[2][FN];
 #pragma unroll
         for (int i = 0; i < 2; ++i)
@@ -251,7 +262,7 @@ gated_wide_kernel(const WideArgs a)
             for (int j = 0; j < FN; ++j)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
-        for (int s = 0; s < steps; ++s) {
+        for (int s = 0; s < blocks; ++s) {
             const uint32_t w_base = base + w_stage * W_BYTES, x_base = base + x_stage * C::X_BYTES;
             w_stage ^= 1;                              // the next block's weights
             const int x_fill = x_stage == 0 ? X_STAGES - 1 : x_stage - 1;       // the next but one's tokens
@@ -290,18 +301,42 @@ gated_wide_kernel(const WideArgs a)
             });
             if (!late) wait_loads<0>();
             __builtin_amdgcn_sched_barrier(0);
-            if (!(late && s + 1 == steps && v + stride >= v_end)) workgroup_barrier();
+            if (!(late && s + 1 == blocks && v + stride >= v_end)) workgroup_barrier();
             __builtin_amdgcn_sched_barrier(0);
         }
 
         // ---- out: lane l holds token l % 32 and, in register 4 q + e, row 8 q + 4 (l / 32) + e of each 32 x 32 block.  The
         // halves of the wavefront trade their columns of every other eight, so that a lane stores 16 bytes of a row and two
         // lanes 32.
-        int rt, tt;
-        place(v, rt, tt);
+        int rt, tt, slice;
+        place(v, rt, tt, slice);
         const int64_t t0 = int64_t(tt) * C::TOKENS;
         const int width = FORWARD ? a.hidden : a.c_in;
         const int n0 = rt * per_tile + wm * (FORWARD ? 32 : 64);
+        if constexpr (SLICED) {                        // partial sums, as they are
+            const int64_t pitch = FORWARD ? 2 * int64_t(width) : width;
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < FN; ++j) {
+                    const int64_t t = t0 + wn * 32 * FN + j * 32 + row;
+                    if (t >= a.tokens) continue;
+                    float *to = a.partial + (int64_t(slice) * a.tokens + t) * pitch + (FORWARD ? i * width : 0);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const int c = n0 + (FORWARD ? 0 : i * 32) + q * 8 + half * 4;
+                        if (width % 4 == 0) {
+                            if (c < width)
+                                *reinterpret_cast<f32x4 *>(to + c) = f32x4{acc[i][j][q * 4], acc[i][j][q * 4 + 1], acc[i][j][q * 4 + 2], acc[i][j][q * 4 + 3]};
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                if (c + e < width) to[c + e] = acc[i][j][q * 4 + e];
+                        }
+                    }
+                }
+            continue;
+        }
         auto store_block = [&](const float (&x)[16], void *out, int64_t pitch, int64_t at, int n, int j) {
             const int64_t t = t0 + wn * 32 * FN + j * 32 + row;
             uint16_t *to = static_cast<uint16_t *>(out) + t * pitch + at;
@@ -374,58 +409,72 @@ gated_wide_kernel(const WideArgs a)
     wait_loads<0>();                                   // nothing may still be writing LDS
 }
 
-template <bool FORWARD, int FN>
+template <bool FORWARD, int FN, bool SLICED>
 dropit_status launch(WideArgs a, hipStream_t stream)
 {
     using C = Wide<FN>;
     constexpr int per_tile = FORWARD ? WIDE_ROWS / 2 : WIDE_ROWS;
     static std::atomic<uint64_t> done{0};
     if (!once_per_device(done, [] {
-            return hipFuncSetAttribute(reinterpret_cast<const void *>(gated_wide_kernel<FORWARD, FN>),
+            return hipFuncSetAttribute(reinterpret_cast<const void *>(gated_wide_kernel<FORWARD, FN, SLICED>),
                                        hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS_BYTES) == hipSuccess;
         }))
         return DROPIT_EHIP;
     a.row_tiles = ((FORWARD ? a.hidden : a.c_in) + per_tile - 1) / per_tile;
     a.token_tiles = int((a.tokens + C::TOKENS - 1) / C::TOKENS);
-    const int64_t tiles = int64_t(a.row_tiles) * a.token_tiles;
+    const int64_t tiles = int64_t(a.row_tiles) * a.token_tiles * a.splits;
     const uint32_t grid = static_cast<uint32_t>(std::min<int64_t>((tiles + 7) / 8 * 8, 256));       // one per compute unit
-    gated_wide_kernel<FORWARD, FN><<<grid, WIDE_THREADS, C::LDS_BYTES, stream>>>(a);
+    gated_wide_kernel<FORWARD, FN, SLICED><<<grid, WIDE_THREADS, C::LDS_BYTES, stream>>>(a);
     return launch_status();
+}
+
+template <bool FORWARD, int FN>
+dropit_status launch(const WideArgs &a, hipStream_t stream)
+{
+    return a.splits > 1 ? launch<FORWARD, FN, true>(a, stream) : launch<FORWARD, FN, false>(a, stream);
 }
 
 }  // namespace
 
-bool gated_wide_takes(int64_t tokens, int c_in, int hidden, bool forward)
+WidePlan gated_wide_plan(int64_t tokens, int64_t c_in, int64_t hidden, bool forward)
 {
     // rows in 16-byte units; the weights, and 256 tokens, below 2^31 bytes
-    return tokens >= 128 && c_in % 8 == 0 && (forward || hidden % 4 == 0) && 4 * int64_t(hidden) * c_in < int64_t(1) << 31 &&
-           std::max(c_in, 2 * hidden) < 1 << 22;
-}
-
-dropit_status launch_gated_wide(const WideArgs &a, bool forward, hipStream_t stream)
-{
-    // How many tokens to a tile: what the compute unit with the most tiles takes, a block of the sum and a tile's start and
-    // end at what they were measured to cost (us; whole chip busy: blocks of 8192 tokens 4096 -> 10240 both ways, ends of
-    // ViT-B's and DeiT-S's forward passes).  Fewer tokens cost more LDS reads per matrix instruction: 64 of them as much as 128
-    // per block, so there is no such tile.  us for 256, 192 and 128 tokens: 12608 tokens 768 -> 2048 forward 109, 105, 123,
-    // backward 81, 74, 108; 25216 tokens 384 -> 1024 75, 73, 77 and 50, 67, 59; 2048 tokens 2048 -> 5632 93, 84, 93 and
-    // 169, 137, 128; 8192 tokens 4096 -> 10240 1004, 1095, 1365.
+    WidePlan plan{tokens > 64 && c_in % 8 == 0 && (forward || hidden % 4 == 0) && 4 * hidden * c_in < int64_t(1) << 31 &&
+                      std::max(c_in, 2 * hidden) < 1 << 22,
+                  2, 1};
+    if (!plan.takes) return plan;
+    // How many tokens to a tile, and how many slices of the sum: what the compute unit with the most tiles takes, a block of
+    // the sum and a tile's start and end at what they were measured to cost (us; whole chip busy: blocks of 8192 tokens 4096 ->
+    // 10240 both ways, ends of ViT-B's and DeiT-S's forward passes).  Fewer tokens cost more LDS reads per matrix instruction:
+    // 64 of them as much as 128 per block, so there is no such tile.  us for 256, 192 and 128 tokens: 12608 tokens 768 -> 2048
+    // forward 109, 105, 123, backward 81, 74, 108; 25216 tokens 384 -> 1024 75, 73, 77 and 50, 67, 59; 2048 tokens 2048 ->
+    // 5632 93, 84, 93 and 169, 137, 128; 8192 tokens 4096 -> 10240 1004, 1095, 1365.  Slices cost a launch and their partial
+    // sums' way to memory and back.
     constexpr double block_us[3] = {1.07, 1.22, 1.57}, end_us[3] = {4.7, 6.3, 8.0};
-    const int64_t rows = forward ? (a.hidden + WIDE_ROWS / 2 - 1) / (WIDE_ROWS / 2) : (a.c_in + WIDE_ROWS - 1) / WIDE_ROWS;
-    const int64_t blocks = (a.K + WIDE_K - 1) / WIDE_K;
-    int best = 0;
+    const int64_t rows = forward ? (hidden + WIDE_ROWS / 2 - 1) / (WIDE_ROWS / 2) : (c_in + WIDE_ROWS - 1) / WIDE_ROWS;
+    const int64_t blocks = ((forward ? c_in : 2 * hidden) + WIDE_K - 1) / WIDE_K;
+    const double slice_us = double(tokens) * double(forward ? 2 * hidden : c_in) * 8 / 4e6;         // 4 bytes out and in at 4 TB/s
     double best_us = 0.0;
     for (int f = 0; f < 3; ++f) {
-        const int64_t tiles = rows * ((a.tokens + 64 * (f + 2) - 1) / (64 * (f + 2)));
-        const int64_t rounds = ((tiles + 7) / 8 + 31) / 32;         // of 32 compute units on each of 8 XCDs
-        const double us = double(rounds) * (double(blocks) * block_us[f] + end_us[f]);
-        if (f == 0 || us <= best_us) {
-            best = f;
-            best_us = us;
+        const int64_t tiles = rows * ((tokens + 64 * (f + 2) - 1) / (64 * (f + 2)));
+        for (int splits = 1; splits <= 16 && (splits == 1 || (tiles * splits <= 512 && blocks / splits >= 8)); ++splits) {
+            const int64_t rounds = ((tiles * splits + 7) / 8 + 31) / 32;        // of 32 compute units on each of 8 XCDs
+            const double us = double(rounds) * (double((blocks + splits - 1) / splits) * block_us[f] + end_us[f]) +
+                              (splits > 1 ? 5.0 + splits * slice_us : 0.0);
+            if (best_us == 0.0 || us < best_us || (us == best_us && splits == 1)) {
+                plan.fn = f + 2;
+                plan.splits = splits;
+                best_us = us;
+            }
         }
     }
-    if (best == 2) return forward ? launch<true, 4>(a, stream) : launch<false, 4>(a, stream);
-    if (best == 1) return forward ? launch<true, 3>(a, stream) : launch<false, 3>(a, stream);
+    return plan;
+}
+
+dropit_status launch_gated_wide(const WideArgs &a, const WidePlan &plan, bool forward, hipStream_t stream)
+{
+    if (plan.fn == 4) return forward ? launch<true, 4>(a, stream) : launch<false, 4>(a, stream);
+    if (plan.fn == 3) return forward ? launch<true, 3>(a, stream) : launch<false, 3>(a, stream);
     return forward ? launch<true, 2>(a, stream) : launch<false, 2>(a, stream);
 }
 
