@@ -1,12 +1,14 @@
 """MI355X-native DropIT hot path: min-k compress + weight gradient from the sparse cache.
 
 The compute lives in ``libdropit.so`` (hand-written gfx950 HIP behind a C ABI,
-declared in ``include/dropit.h``).  This package is only the ctypes binding:
+declared in ``include/dropit.h``; the operators beside the cache in a training step,
+gated projection, AdamW and gradient norm, in ``include/dropit_layers.h``).  This package is only the ctypes binding:
 argument marshalling from torch tensors (device memory + streams) to raw
 pointers.  There is no CPU fallback: without the built library, or without a
 GPU, the calls raise.
 """
-from . import nn  # noqa: F401  (autograd wrappers: nn.Linear, nn.Conv2d, nn.apply_dropit)
+from . import nn  # noqa: F401  (autograd wrappers: nn.Linear, nn.Conv2d, nn.GatedLinear, nn.apply_dropit)
+from . import optim  # noqa: F401  (optim.AdamW)
 from .binding import (  # noqa: F401
     DropitError,
     compress,

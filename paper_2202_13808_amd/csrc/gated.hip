@@ -19,6 +19,8 @@ typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(16))) float f32x16;
+// sixteen bytes at any element's address: a row of odd length moves in wide accesses too
+typedef u32x4 u32x4_any __attribute__((aligned(2)));
 
 template <bool BF16> struct Elem { using type = float; static constexpr int PER16 = 4; };
 template <> struct Elem<true> { using type = uint16_t; static constexpr int PER16 = 8; };
@@ -36,7 +38,7 @@ template <bool BF16> __device__ inline void store_one(void *p, int64_t i, float 
 
 // ---------------------------------------------------------------------------
 // The product for every size and type: tiles of 64 tokens by 128 rows of the weight operand, four wavefronts of 64 x 32.
-// fp32 runs on the fp32 matrix instructions.  Rows whose length is no multiple of 16 bytes load element by element.
+// fp32 runs on the fp32 matrix instructions.
 // Few tiles: the sum is cut into slices, whose partial sums finish_kernel adds in ascending order.
 constexpr int GEN_THREADS = 256, GEN_ROWS = 128, GEN_TOKENS = 64, GEN_K = 32;
 
@@ -53,12 +55,12 @@ struct GenArgs {
 };
 
 // sixteen bytes of row `row` of a K-contiguous operand from element k on, zeros past the end
-template <bool BF16, bool VEC>
+template <bool BF16>
 __device__ inline u32x4 load_unit(const void *base, int64_t row, int64_t pitch, int k, int end)
 {
     constexpr int PER = Elem<BF16>::PER16;
     const auto *p = static_cast<const typename Elem<BF16>::type *>(base) + row * pitch + k;
-    if (VEC && k + PER <= end) return *reinterpret_cast<const u32x4 *>(p);
+    if (k + PER <= end) return *reinterpret_cast<const u32x4_any *>(p);
     u32x4 r = {0u, 0u, 0u, 0u};
 #pragma unroll
     for (int e = 0; e < PER; ++e)
@@ -69,7 +71,7 @@ __device__ inline u32x4 load_unit(const void *base, int64_t row, int64_t pitch, 
     return r;
 }
 
-template <bool BF16, bool FORWARD, bool VEC>
+template <bool BF16, bool FORWARD>
 __global__ void __launch_bounds__(GEN_THREADS)
 gated_product_kernel(const GenArgs a)
 {
@@ -77,7 +79,12 @@ gated_product_kernel(const GenArgs a)
     constexpr int UNITS = GEN_K / PER;                              // 16-byte units of a tile row
     constexpr int PITCH = GEN_K * ES + 16;                          // bytes of an LDS row: the pad spreads the rows over the banks
     constexpr int A_LOADS = GEN_ROWS * UNITS / GEN_THREADS, B_LOADS = GEN_TOKENS * UNITS / GEN_THREADS;
-    __shared__ __attribute__((aligned(16))) char tile[2][(GEN_ROWS + GEN_TOKENS) * PITCH];
+    // The input gradient's weights arrive along the columns, [k][column].  In fp32 a matrix instruction takes one k at a time
+    // and reads them as they lie; in bf16 it takes eight, and they are turned on the way into LDS.
+    constexpr bool AS_IT_LIES = !FORWARD && !BF16;
+    constexpr int K_PITCH = GEN_ROWS * ES + 16;
+    constexpr int A_BYTES = AS_IT_LIES ? GEN_K * K_PITCH : GEN_ROWS * PITCH;
+    __shared__ __attribute__((aligned(16))) char tile[2][A_BYTES + GEN_TOKENS * PITCH];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int wm = wave >> 1, wn = wave & 1;
     const int rt = int(blockIdx.x % unsigned(a.row_tiles));
@@ -99,16 +106,16 @@ gated_product_kernel(const GenArgs a)
         for (int i = 0; i < A_LOADS; ++i) {
             const int unit = i * GEN_THREADS + tid;
             if constexpr (FORWARD) {
-                ra[i] = load_unit<BF16, VEC>(a.w, weight_row(unit / UNITS), a.c_in, k0 + unit % UNITS * PER, a.K);
+                ra[i] = load_unit<BF16>(a.w, weight_row(unit / UNITS), a.c_in, k0 + unit % UNITS * PER, a.K);
             } else {                                                // W [K][c_in]: a unit is PER columns of one k
                 const int k = k0 + unit / (GEN_ROWS / PER), c = r0 + unit % (GEN_ROWS / PER) * PER;
-                ra[i] = k < a.K && c < a.c_in ? load_unit<BF16, VEC>(a.w, k, a.c_in, c, a.c_in) : u32x4{0u, 0u, 0u, 0u};
+                ra[i] = k < a.K && c < a.c_in ? load_unit<BF16>(a.w, k, a.c_in, c, a.c_in) : u32x4{0u, 0u, 0u, 0u};
             }
         }
 #pragma unroll
         for (int i = 0; i < B_LOADS; ++i) {
             const int unit = i * GEN_THREADS + tid;
-            rb[i] = load_unit<BF16, VEC>(a.x, min<int64_t>(t0 + unit / UNITS, a.tokens - 1), a.K, k0 + unit % UNITS * PER, a.K);
+            rb[i] = load_unit<BF16>(a.x, min<int64_t>(t0 + unit / UNITS, a.tokens - 1), a.K, k0 + unit % UNITS * PER, a.K);
         }
     };
     auto put = [&](char *to) {
@@ -119,18 +126,19 @@ gated_product_kernel(const GenArgs a)
                 *reinterpret_cast<u32x4 *>(to + unit / UNITS * PITCH + unit % UNITS * 16) = ra[i];
             } else {
                 const int k = unit / (GEN_ROWS / PER), c = unit % (GEN_ROWS / PER) * PER;
+                if constexpr (AS_IT_LIES) *reinterpret_cast<u32x4 *>(to + k * K_PITCH + c * ES) = ra[i];
+                else
 #pragma unroll
                 for (int e = 0; e < PER; ++e) {
                     char *at = to + (c + e) * PITCH + k * ES;
-                    if constexpr (BF16) *reinterpret_cast<uint16_t *>(at) = uint16_t(ra[i][e >> 1] >> (16 * (e & 1)));
-                    else *reinterpret_cast<uint32_t *>(at) = ra[i][e];
+                    *reinterpret_cast<uint16_t *>(at) = uint16_t(ra[i][e >> 1] >> (16 * (e & 1)));
                 }
             }
         }
 #pragma unroll
         for (int i = 0; i < B_LOADS; ++i) {
             const int unit = i * GEN_THREADS + tid;
-            *reinterpret_cast<u32x4 *>(to + (GEN_ROWS + unit / UNITS) * PITCH + unit % UNITS * 16) = rb[i];
+            *reinterpret_cast<u32x4 *>(to + A_BYTES + unit / UNITS * PITCH + unit % UNITS * 16) = rb[i];
         }
     };
 
@@ -145,7 +153,7 @@ gated_product_kernel(const GenArgs a)
         put(cur);
         __syncthreads();                                            // (the other tile's readers passed the barrier before)
         if (s + 1 < s1) load(s + 1);
-        const char *wa = cur + (wm * 64 + (lane & 31)) * PITCH, *xb = cur + (GEN_ROWS + wn * 32 + (lane & 31)) * PITCH;
+        const char *wa = cur + (wm * 64 + (lane & 31)) * PITCH, *xb = cur + A_BYTES + (wn * 32 + (lane & 31)) * PITCH;
         if constexpr (BF16) {
 #pragma unroll
             for (int kk = 0; kk < GEN_K / 16; ++kk) {
@@ -163,7 +171,15 @@ gated_product_kernel(const GenArgs a)
                 const f32x4 b = *reinterpret_cast<const f32x4 *>(xb + at);
                 f32x4 w[2];
 #pragma unroll
-                for (int i = 0; i < 2; ++i) w[i] = *reinterpret_cast<const f32x4 *>(wa + i * 32 * PITCH + at);
+                for (int i = 0; i < 2; ++i) {
+                    if constexpr (AS_IT_LIES) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            w[i][e] = *reinterpret_cast<const float *>(cur + (kk * 8 + (lane >> 5) * 4 + e) * K_PITCH + (wm * 64 + i * 32 + (lane & 31)) * ES);
+                    } else {
+                        w[i] = *reinterpret_cast<const f32x4 *>(wa + i * 32 * PITCH + at);
+                    }
+                }
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
 #pragma unroll
@@ -271,10 +287,7 @@ dropit_status launch_generic(GenArgs a, hipStream_t stream)
     if (a.splits == 1) a.partial = nullptr;
     const int64_t tiles = (a.tokens + GEN_TOKENS - 1) / GEN_TOKENS * a.row_tiles;
     const dim3 grid(static_cast<uint32_t>(tiles), a.splits);
-    // whole rows in 16-byte units: both operands' row lengths allow it
-    const bool vec = a.c_in % Elem<BF16>::PER16 == 0 && a.K % Elem<BF16>::PER16 == 0;
-    if (vec) gated_product_kernel<BF16, FORWARD, true><<<grid, GEN_THREADS, 0, stream>>>(a);
-    else gated_product_kernel<BF16, FORWARD, false><<<grid, GEN_THREADS, 0, stream>>>(a);
+    gated_product_kernel<BF16, FORWARD><<<grid, GEN_THREADS, 0, stream>>>(a);
     if (a.splits > 1) launch_finish<BF16, FORWARD>(a, stream);
     return launch_status();
 }
@@ -305,72 +318,85 @@ dropit_status launch_wide(GenArgs a, const WidePlan &plan, hipStream_t stream)
 // ---------------------------------------------------------------------------
 // dpre from dh and pre, and the partial column sums for dbias.  A thread takes 8 (bf16) or 4 (fp32) gate columns, the up
 // columns beside them and every fourth row of a block of rows; the four row groups' sums meet in LDS.
-constexpr int SLOPE_LANES = 64, SLOPE_GROUPS = 4, SLOPE_ROWS = 64;
+constexpr int SLOPE_LANES = 64, SLOPE_GROUPS = 4, SLOPE_ROWS_MOST = 64;
 
-template <bool BF16, bool VEC>
+template <bool BF16>
 __global__ void __launch_bounds__(SLOPE_LANES * SLOPE_GROUPS)
-gated_slope_kernel(const void *__restrict__ dh, const void *__restrict__ pre, int64_t tokens, int hidden, int act,
+gated_slope_kernel(const void *__restrict__ dh, const void *__restrict__ pre, int64_t tokens, int hidden, int rows, int act,
                    void *__restrict__ dpre, float *__restrict__ partial /* [row blocks][2 * hidden] or null */)
 {
-    constexpr int PER = VEC ? Elem<BF16>::PER16 : 1;
+    constexpr int PER = Elem<BF16>::PER16;
+    using T = typename Elem<BF16>::type;
     __shared__ float red[SLOPE_GROUPS][SLOPE_LANES * PER * 2];
     const int lane = threadIdx.x % SLOPE_LANES, group = threadIdx.x / SLOPE_LANES;
     const int n = int(blockIdx.x * SLOPE_LANES + lane) * PER;
-    const int64_t t0 = int64_t(blockIdx.y) * SLOPE_ROWS, t1 = min<int64_t>(t0 + SLOPE_ROWS, tokens);
+    const int64_t t0 = int64_t(blockIdx.y) * rows, t1 = min<int64_t>(t0 + rows, tokens);
     float sg[PER], su[PER];
 #pragma unroll
     for (int e = 0; e < PER; ++e) sg[e] = su[e] = 0.f;
+    auto widen = [](const u32x4 &r, float (&x)[PER]) {
+#pragma unroll
+        for (int e = 0; e < PER; ++e) {
+            if constexpr (BF16) x[e] = __uint_as_float((e & 1) ? r[e >> 1] & 0xffff0000u : r[e >> 1] << 16);
+            else x[e] = __uint_as_float(r[e]);
+        }
+    };
+    auto narrow = [](const float (&x)[PER]) {
+        u32x4 r;
+        if constexpr (BF16) {
+            bf16x8 b;
+#pragma unroll
+            for (int e = 0; e < PER; ++e) b[e] = static_cast<__bf16>(x[e]);
+            r = __builtin_bit_cast(u32x4, b);
+        } else {
+#pragma unroll
+            for (int e = 0; e < PER; ++e) r[e] = __float_as_uint(x[e]);
+        }
+        return r;
+    };
     if (n < hidden) {
+        const bool whole = n + PER <= hidden;
 #pragma unroll 2
         for (int64_t t = t0 + group; t < t1; t += SLOPE_GROUPS) {
-            const int64_t ih = t * hidden + n, ig = t * 2 * hidden + n, iu = ig + hidden;
+            const T *pd = static_cast<const T *>(dh) + t * hidden + n, *pg = static_cast<const T *>(pre) + t * 2 * hidden + n;
+            T *og = static_cast<T *>(dpre) + t * 2 * hidden + n;
             float d[PER], g[PER], u[PER];
-            if constexpr (VEC) {
-                using T = typename Elem<BF16>::type;
-                const u32x4 rd = *reinterpret_cast<const u32x4 *>(static_cast<const T *>(dh) + ih);
-                const u32x4 rg = *reinterpret_cast<const u32x4 *>(static_cast<const T *>(pre) + ig);
-                const u32x4 ru = *reinterpret_cast<const u32x4 *>(static_cast<const T *>(pre) + iu);
+            if (whole) {
+                const u32x4 rd = *reinterpret_cast<const u32x4_any *>(pd), rg = *reinterpret_cast<const u32x4_any *>(pg),
+                            ru = *reinterpret_cast<const u32x4_any *>(pg + hidden);
+                widen(rd, d);
+                widen(rg, g);
+                widen(ru, u);
+            } else {
 #pragma unroll
                 for (int e = 0; e < PER; ++e) {
-                    if constexpr (BF16) {
-                        d[e] = __uint_as_float((e & 1) ? rd[e >> 1] & 0xffff0000u : rd[e >> 1] << 16);
-                        g[e] = __uint_as_float((e & 1) ? rg[e >> 1] & 0xffff0000u : rg[e >> 1] << 16);
-                        u[e] = __uint_as_float((e & 1) ? ru[e >> 1] & 0xffff0000u : ru[e >> 1] << 16);
-                    } else {
-                        d[e] = __uint_as_float(rd[e]);
-                        g[e] = __uint_as_float(rg[e]);
-                        u[e] = __uint_as_float(ru[e]);
+                    d[e] = g[e] = u[e] = 0.f;
+                    if (n + e < hidden) {
+                        d[e] = load_one<BF16>(pd, e);
+                        g[e] = load_one<BF16>(pg, e);
+                        u[e] = load_one<BF16>(pg + hidden, e);
                     }
                 }
-            } else {
-                d[0] = load_one<BF16>(dh, ih);
-                g[0] = load_one<BF16>(pre, ig);
-                u[0] = load_one<BF16>(pre, iu);
             }
+            float slope[PER];
+            activation_slopes<BF16>(g, act, slope);    // g becomes act(g)
 #pragma unroll
             for (int e = 0; e < PER; ++e) {
-                float slope;
-                const float value = activation_slope<BF16>(g[e], act, slope);
-                g[e] = d[e] * u[e] * slope;
-                u[e] = d[e] * value;
-                sg[e] += g[e];
-                su[e] += u[e];
+                u[e] = d[e] * u[e] * slope[e];
+                g[e] = d[e] * g[e];
+                sg[e] += u[e];
+                su[e] += g[e];
             }
-            if constexpr (VEC && BF16) {
-                bf16x8 og, ou;
-#pragma unroll
-                for (int e = 0; e < PER; ++e) {
-                    og[e] = static_cast<__bf16>(g[e]);
-                    ou[e] = static_cast<__bf16>(u[e]);
-                }
-                *reinterpret_cast<bf16x8 *>(static_cast<uint16_t *>(dpre) + ig) = og;
-                *reinterpret_cast<bf16x8 *>(static_cast<uint16_t *>(dpre) + iu) = ou;
-            } else if constexpr (VEC) {
-                *reinterpret_cast<f32x4 *>(static_cast<float *>(dpre) + ig) = f32x4{g[0], g[1], g[2], g[3]};
-                *reinterpret_cast<f32x4 *>(static_cast<float *>(dpre) + iu) = f32x4{u[0], u[1], u[2], u[3]};
+            if (whole) {
+                *reinterpret_cast<u32x4_any *>(og) = narrow(u);
+                *reinterpret_cast<u32x4_any *>(og + hidden) = narrow(g);
             } else {
-                store_one<BF16>(dpre, ig, g[0]);
-                store_one<BF16>(dpre, iu, u[0]);
+#pragma unroll
+                for (int e = 0; e < PER; ++e)
+                    if (n + e < hidden) {
+                        store_one<BF16>(og, e, u[e]);
+                        store_one<BF16>(og + hidden, e, g[e]);
+                    }
             }
         }
     }
@@ -407,7 +433,19 @@ gated_bias_kernel(const float *__restrict__ partial, int64_t blocks, int64_t wid
     dbias[n] = s;
 }
 
-int64_t row_blocks(int64_t tokens) { return (tokens + SLOPE_ROWS - 1) / SLOPE_ROWS; }
+// columns of the slope kernel's workgroups, and the rows of each: 64 where that still leaves four workgroups to a compute unit,
+// fewer for fewer tokens (64 tokens of 1024 columns took 16 us as one block of rows, one row after the other)
+int64_t slope_strips(int64_t hidden, dropit_dtype dt)
+{
+    const int64_t per = dt == DROPIT_BF16 ? 8 : 4;
+    return ((hidden + per - 1) / per + SLOPE_LANES - 1) / SLOPE_LANES;
+}
+int64_t slope_rows(int64_t tokens, int64_t hidden, dropit_dtype dt)
+{
+    const int64_t wanted = tokens * slope_strips(hidden, dt) / 1024;
+    return std::min<int64_t>(SLOPE_ROWS_MOST, std::max<int64_t>(SLOPE_GROUPS, wanted / SLOPE_GROUPS * SLOPE_GROUPS));
+}
+int64_t row_blocks(int64_t tokens, int64_t rows) { return (tokens + rows - 1) / rows; }
 
 bool valid_sizes(int64_t tokens, int64_t c_in, int64_t hidden, dropit_dtype dt)
 {
@@ -480,7 +518,7 @@ extern "C" size_t dropit_gated_backward_workspace_bytes(int64_t tokens, int64_t 
 {
     if (!valid_sizes(tokens, c_in, hidden, dt)) return 0;
     size_t need = need_dx ? dx_bytes(tokens, c_in, hidden, dt) : 0;
-    if (need_dbias) need = std::max(need, size_t(row_blocks(tokens)) * 2 * hidden * sizeof(float));
+    if (need_dbias) need = std::max(need, size_t(row_blocks(tokens, slope_rows(tokens, hidden, dt))) * 2 * hidden * sizeof(float));
     return need;
 }
 
@@ -500,30 +538,21 @@ extern "C" dropit_status dropit_gated_backward(const void *dh, const void *pre, 
     const bool bf16 = dt == DROPIT_BF16;
     // the partial column sums and, when those are added, dx's slices share the workspace, one after the other
     float *partial = dbias != nullptr ? static_cast<float *>(workspace) : nullptr;
-    if (tokens > 0) {
-        const bool vec = hidden % (bf16 ? 8 : 4) == 0;
-        const int64_t cols = vec ? hidden / (bf16 ? 8 : 4) : hidden;
-        const int64_t strips = (cols + SLOPE_LANES - 1) / SLOPE_LANES;
-        // the grid's second dimension holds 65535 row blocks: more tokens go in several launches
-        for (int64_t b0 = 0; b0 < row_blocks(tokens); b0 += 65535) {
-            const int64_t first = b0 * SLOPE_ROWS, some = std::min<int64_t>(tokens - first, int64_t(65535) * SLOPE_ROWS);
-            const dim3 grid(static_cast<uint32_t>(strips), static_cast<uint32_t>(row_blocks(some)));
-            const size_t es = bf16 ? 2 : 4;
-            const char *d = static_cast<const char *>(dh) + first * hidden * es;
-            const char *p = static_cast<const char *>(pre) + first * 2 * hidden * es;
-            char *o = static_cast<char *>(dpre) + first * 2 * hidden * es;
-            float *part = partial != nullptr ? partial + b0 * 2 * hidden : nullptr;
-            auto launch = [&](auto kernel) {
-                kernel<<<grid, SLOPE_LANES * SLOPE_GROUPS, 0, stream>>>(d, p, some, int(hidden), act, o, part);
-            };
-            if (bf16 && vec) launch(gated_slope_kernel<true, true>);
-            else if (bf16) launch(gated_slope_kernel<true, false>);
-            else if (vec) launch(gated_slope_kernel<false, true>);
-            else launch(gated_slope_kernel<false, false>);
-        }
+    const int64_t rows = slope_rows(tokens, hidden, dt), blocks = row_blocks(tokens, rows);
+    // the grid's second dimension holds 65535 row blocks: more tokens go in several launches
+    for (int64_t b0 = 0; b0 < blocks; b0 += 65535) {
+        const int64_t first = b0 * rows, some = std::min<int64_t>(tokens - first, int64_t(65535) * rows);
+        const dim3 grid(static_cast<uint32_t>(slope_strips(hidden, dt)), static_cast<uint32_t>(row_blocks(some, rows)));
+        const size_t es = bf16 ? 2 : 4;
+        const char *d = static_cast<const char *>(dh) + first * hidden * es;
+        const char *p = static_cast<const char *>(pre) + first * 2 * hidden * es;
+        char *o = static_cast<char *>(dpre) + first * 2 * hidden * es;
+        float *part = partial != nullptr ? partial + b0 * 2 * hidden : nullptr;
+        if (bf16) gated_slope_kernel<true><<<grid, SLOPE_LANES * SLOPE_GROUPS, 0, stream>>>(d, p, some, int(hidden), int(rows), act, o, part);
+        else gated_slope_kernel<false><<<grid, SLOPE_LANES * SLOPE_GROUPS, 0, stream>>>(d, p, some, int(hidden), int(rows), act, o, part);
     }
     if (dbias != nullptr)
-        gated_bias_kernel<<<static_cast<uint32_t>((2 * hidden + 15) / 16), 256, 0, stream>>>(partial, row_blocks(tokens), 2 * hidden, dbias);
+        gated_bias_kernel<<<static_cast<uint32_t>((2 * hidden + 15) / 16), 256, 0, stream>>>(partial, blocks, 2 * hidden, dbias);
     if (dx == nullptr || tokens == 0) return launch_status();
     GenArgs a{};
     a.w = w;

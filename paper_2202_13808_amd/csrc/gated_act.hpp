@@ -97,5 +97,21 @@ template <bool FAST> __device__ inline float activation_slope(float z, int act, 
     }
 }
 
+// the same over N values: act(z) in place of z, act'(z) in `slope`
+template <bool FAST, int N> __device__ inline void activation_slopes(float (&z)[N], int act, float (&slope)[N])
+{
+    auto each = [&](auto code) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) z[i] = activation_slope<FAST>(z[i], decltype(code)::value, slope[i]);
+    };
+    switch (act) {
+    case DROPIT_ACT_SILU: return each(std::integral_constant<int, DROPIT_ACT_SILU>{});
+    case DROPIT_ACT_GELU: return each(std::integral_constant<int, DROPIT_ACT_GELU>{});
+    case DROPIT_ACT_GELU_TANH: return each(std::integral_constant<int, DROPIT_ACT_GELU_TANH>{});
+    case DROPIT_ACT_RELU: return each(std::integral_constant<int, DROPIT_ACT_RELU>{});
+    default: return each(std::integral_constant<int, DROPIT_ACT_SIGMOID>{});
+    }
+}
+
 }  // namespace
 }  // namespace dropit

@@ -438,8 +438,10 @@ dropit_status launch(const WideArgs &a, hipStream_t stream)
 
 WidePlan gated_wide_plan(int64_t tokens, int64_t c_in, int64_t hidden, bool forward)
 {
-    // rows in 16-byte units; the weights, and 256 tokens, below 2^31 bytes
-    WidePlan plan{tokens > 64 && c_in % 8 == 0 && (forward || hidden % 4 == 0) && 4 * hidden * c_in < int64_t(1) << 31 &&
+    // rows in 16-byte units; the weights, and 256 tokens, below 2^31 bytes.  Few tokens leave most of a tile empty, but its
+    // slices fill the chip (us for the gradients of 16 tokens, here and in gated.hip's product: 384 -> 1024 15 and 19, 2048 ->
+    // 5632 23 and 46, 4096 -> 10240 45 and 115)
+    WidePlan plan{(!forward || tokens > 32) && c_in % 8 == 0 && (forward || hidden % 4 == 0) && 4 * hidden * c_in < int64_t(1) << 31 &&
                       std::max(c_in, 2 * hidden) < 1 << 22,
                   2, 1};
     if (!plan.takes) return plan;

@@ -24,7 +24,7 @@ from typing import Iterator, List, Optional, Sequence, Tuple, Union
 import torch
 import torch.nn.functional as F
 
-from . import binding
+from . import binding, layers
 
 _Int2 = Union[int, Sequence[int]]
 
@@ -208,6 +208,79 @@ def conv2d(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] =
 
 
 # ---------------------------------------------------------------------------------------------
+# gated projection of a feed-forward block: a fully-connected layer of twice the width whose two halves, a gate and an up
+# projection, meet in one elementwise product.  Its weight gradient is the fully-connected one (Sec. 3.2, Eq.
+# fc_backward_elem_save) on the same cache of the input; the activation's input is kept whole, as Sec. 3.5 leaves activations.
+# ---------------------------------------------------------------------------------------------
+def _contiguous(t: torch.Tensor) -> torch.Tensor:
+    return t if t.is_contiguous() and t.data_ptr() % 16 == 0 else t.clone(memory_format=torch.contiguous_format)
+
+
+class _GatedFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, act, gamma, seed, fmt):
+        xc, wc = _contiguous(x.detach()), _contiguous(weight.detach())
+        h, pre = layers.gated_forward(xc, wc, _contiguous(bias.detach()) if bias is not None else None, act=act, save=True)
+        cache = ()
+        if ctx.needs_input_grad[1]:
+            cache = _compress_input(xc, gamma, seed, fmt) if gamma > 0.0 else (xc,)
+        ctx.save_for_backward(wc, pre, *cache)
+        ctx.act, ctx.gamma, ctx.fmt = act, gamma, fmt
+        ctx.x_shape = tuple(x.shape)
+        ctx.bias_dtype = bias.dtype if bias is not None else None
+        return h
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dh):
+        weight, pre, *cache = ctx.saved_tensors
+        need_x, need_w, need_b = ctx.needs_input_grad[:3]
+        dpre, dx, db = layers.gated_backward(_match_dtype(dh, pre), pre, weight, act=ctx.act, need_dx=need_x,
+                                             need_dbias=bool(need_b and ctx.bias_dtype is not None))
+        dw = None
+        if need_w:
+            dpre2 = dpre.reshape(-1, weight.shape[0])
+            if dpre2.shape[0] == 0:
+                dw = torch.zeros_like(weight)
+            elif ctx.gamma > 0.0:
+                dw = _weight_grad(cache, ctx.fmt, ctx.x_shape, dpre2, weight.shape[0]).to(weight.dtype)
+            else:
+                dw = dpre2.t() @ cache[0].reshape(-1, weight.shape[1])
+        return dx, dw, db.to(ctx.bias_dtype) if db is not None else None, None, None, None, None
+
+
+def _gated_plain(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor], act: str) -> torch.Tensor:
+    gate, up = F.linear(x, weight, bias).chunk(2, -1)
+    gate = {"silu": F.silu, "gelu": F.gelu, "gelu_tanh": lambda z: F.gelu(z, approximate="tanh"), "relu": F.relu,
+            "sigmoid": torch.sigmoid}[act](gate)
+    return gate * up
+
+
+def gated_linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, act: str = "silu",
+                 gamma: float = 0.9, seed: Optional[int] = None, index_format: str = "flat") -> torch.Tensor:
+    """``act(x Wg^T + bg) * (x Wu^T + bu)`` with ``weight`` = [Wg; Wu] of shape [2 * hidden, c_in] and ``bias`` [2 * hidden]:
+    both projections, the activation (silu, gelu, gelu_tanh, relu, sigmoid) and the product in one kernel.  The backward pass
+    takes the weight gradient from the min-k cache of ``x`` (``gamma`` = 0 keeps ``x`` itself; ``seed`` and ``index_format``
+    as for ``linear``) and keeps the pre-activations whole.  Under autocast the operands are cast as ``F.linear``'s are."""
+    layers._act_code(act)
+    layers._gated_sizes(weight)
+    _check_format(index_format)
+    if torch.is_autocast_enabled("cuda") and x.is_cuda:
+        dtype = torch.get_autocast_dtype("cuda")
+        x, weight, bias = x.to(dtype), weight.to(dtype), bias.to(dtype) if bias is not None else None
+    if not x.is_cuda:
+        if gamma > 0.0 and torch.is_grad_enabled() and weight.requires_grad:
+            raise RuntimeError("DropIT layers train on device tensors only: there is no CPU path")
+        return _gated_plain(x, weight, bias, act)
+    with torch.autocast("cuda", enabled=False):
+        if not torch.is_grad_enabled() or not any(t is not None and t.requires_grad for t in (x, weight, bias)):
+            return layers.gated_forward(_contiguous(x), _contiguous(weight), _contiguous(bias) if bias is not None else None, act=act)
+        if x.numel() == 0:
+            gamma = 0.0
+        return _GatedFn.apply(x, weight, bias, act, float(gamma), seed, index_format)
+
+
+# ---------------------------------------------------------------------------------------------
 # modules and the layer policy
 # ---------------------------------------------------------------------------------------------
 _SEED_STRIDE = 0x9E3779B97F4A7C15      # odd: successive calls of a layer walk through all 2^64 seeds
@@ -280,13 +353,54 @@ class Conv2d(torch.nn.Conv2d):
         return super().extra_repr() + ", gamma=%g" % self.gamma
 
 
+class GatedLinear(torch.nn.Module):
+    """The gated projection of a feed-forward block (``gated_linear``): in_features -> hidden_features, with one weight
+    [2 * hidden_features, in_features] (gate rows first) and bias [2 * hidden_features].  In training the weight gradient
+    comes from the dropped cache of the input (``gamma`` = 0: from the input itself); inference is unchanged."""
+
+    def __init__(self, in_features: int, hidden_features: int, bias: bool = True, act: str = "silu", gamma: float = 0.9,
+                 strategy: str = "mink", seed: int = 0, index_format: str = "flat", device=None, dtype=None) -> None:
+        super().__init__()
+        layers._act_code(act)
+        self.in_features, self.hidden_features, self.act = int(in_features), int(hidden_features), act
+        self.weight = torch.nn.Parameter(torch.empty(2 * self.hidden_features, self.in_features, device=device, dtype=dtype))
+        if bias:
+            self.bias = torch.nn.Parameter(torch.empty(2 * self.hidden_features, device=device, dtype=dtype))
+        else:
+            self.register_parameter("bias", None)
+        self.gamma = float(gamma)
+        self.strategy = _check_strategy(strategy)
+        self.seed = int(seed)
+        self.index_format = _check_format(index_format)
+        if self.strategy == "random" and self.index_format != "flat":
+            raise ValueError("the random strategy keeps flat indices (index_format='flat')")
+        self.reset_parameters()
+
+    def reset_parameters(self) -> None:
+        bound = self.in_features ** -0.5               # as nn.Linear: uniform within 1 / sqrt(in_features)
+        with torch.no_grad():
+            self.weight.uniform_(-bound, bound)
+            if self.bias is not None:
+                self.bias.uniform_(-bound, bound)
+
+    def forward(self, x: torch.Tensor) -> torch.Tensor:
+        dropping = _dropping(self)
+        return gated_linear(x, self.weight, self.bias, self.act, self.gamma if dropping else 0.0,
+                            _next_seed(self) if dropping else None, self.index_format)
+
+    def extra_repr(self) -> str:
+        return "in_features=%d, hidden_features=%d, bias=%s, act=%s, gamma=%g" % (
+            self.in_features, self.hidden_features, self.bias is not None, self.act, self.gamma)
+
+
 def apply_dropit(model: torch.nn.Module, gamma: float, skip_first: bool = True,
                  skip_last: bool = True, strategy: str = "mink", seed: int = 0,
                  index_format: str = "flat") -> List[str]:
     """Switch the applicable layers of ``model`` to DropIT in place and return their names.
 
-    Applicable: ``nn.Linear`` and ``nn.Conv2d`` (groups = 1, zero padding); the modules keep their
-    parameters, buffers, hooks and state-dict keys (only their class changes).  The first and the
+    Applicable: ``nn.Linear``, ``nn.Conv2d`` (groups = 1, zero padding) and this module's ``GatedLinear``; the
+    modules keep their parameters, buffers, hooks and state-dict keys (only their class changes, and a
+    ``GatedLinear``'s dropping rate).  The first and the
     last applicable layer, in module registration order, are left as they are unless asked
     otherwise: their inputs stay alive (or are created last) whatever the layer caches, so
     dropping there adds the sparse copy to the peak instead of lowering it.  ``strategy`` is
@@ -295,7 +409,7 @@ def apply_dropit(model: torch.nn.Module, gamma: float, skip_first: bool = True,
     offsets instead of int32 flat indices (min-k only)."""
     found: List[Tuple[str, torch.nn.Module]] = []
     for name, m in model.named_modules():
-        if type(m) is torch.nn.Linear or (type(m) is torch.nn.Conv2d and _conv_applicable(m)):
+        if type(m) in (torch.nn.Linear, GatedLinear) or (type(m) is torch.nn.Conv2d and _conv_applicable(m)):
             found.append((name, m))
     if skip_first and found:
         found = found[1:]
@@ -305,7 +419,8 @@ def apply_dropit(model: torch.nn.Module, gamma: float, skip_first: bool = True,
     _check_format(index_format)
     for number, (_, m) in enumerate(found):
         m.index_format = index_format
-        m.__class__ = Linear if isinstance(m, torch.nn.Linear) else Conv2d
+        if not isinstance(m, GatedLinear):
+            m.__class__ = Linear if isinstance(m, torch.nn.Linear) else Conv2d
         m.gamma = float(gamma)
         m.strategy = strategy
         m.seed = (int(seed) + (number << 48)) & 0xFFFFFFFFFFFFFFFF     # layers draw from disjoint seed ranges

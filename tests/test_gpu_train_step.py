@@ -1,0 +1,286 @@
+"""The operators of a training step together, the way a program uses them: nn.GatedLinear with the dropped cache, gradients
+clipped and stepped by optim.AdamW, whole and captured into a graph."""
+import copy
+import io
+import math
+
+import numpy as np
+import pytest
+import torch
+import torch.nn.functional as F
+
+import oracle
+import paper_2202_13808_amd as dropit
+from paper_2202_13808_amd import block_bench
+from paper_2202_13808_amd import nn as dnn
+from dropit_inputs import activation, gradient
+from gpu_util import to_device
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+HALF = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8}
+
+
+def _dropped(x, gamma):
+    """R(a^) of a host array, in fp64."""
+    k = oracle.keep_count(x.size, gamma)
+    vals, idx = oracle.compress(x, k)
+    return torch.from_numpy(oracle.densify(vals, idx, x.shape)).double()
+
+
+@pytest.mark.parametrize("index_format", ["flat", "rows", "mask"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("gamma", [0.9, 0.6, 0.0])
+def test_gated_layer_gradients(gamma, dtype, index_format):
+    print("gated layer", gamma, dtype, index_format, flush=True)
+    tdt = torch.float32 if dtype == "f32" else torch.bfloat16
+    x_h, dy_h = activation((6, 50, 96), "normal", 31, dtype), gradient((6, 50, 40), 0.02, 32, dtype)
+    torch.manual_seed(3)
+    layer = dnn.GatedLinear(96, 40, act="silu", gamma=gamma, index_format=index_format, device=DEV, dtype=tdt)
+    x = to_device(x_h).requires_grad_(True)
+    with dnn.cache_meter() as meter:
+        h = layer(x)
+    assert meter.layers == (1 if gamma > 0 else 0)
+    h.backward(to_device(dy_h))
+    torch.cuda.synchronize()
+    # the formula in 64 bits: everything but the weight gradient from x itself, that from the dropped x
+    w, b = layer.weight.detach().cpu().double(), layer.bias.detach().cpu().double()
+    xs = torch.from_numpy(oracle.widen(x_h)).double().reshape(-1, 96)
+    dy = torch.from_numpy(oracle.widen(dy_h)).double().reshape(-1, 40)
+    pre = (xs @ w.t() + b).requires_grad_(True)
+    ref = F.silu(pre[:, :40]) * pre[:, 40:]
+    (dpre,) = torch.autograd.grad(ref, pre, dy)
+    xd = _dropped(x_h, gamma).reshape(-1, 96) if gamma > 0 else xs
+    want = {"h": ref.detach(), "x": dpre @ w, "w": dpre.t() @ xd, "b": dpre.sum(0)}
+    got = {"h": h.detach().reshape(-1, 40), "x": x.grad.reshape(-1, 96), "w": layer.weight.grad, "b": layer.bias.grad}
+    # bf16: pre and dpre are rounded (relative 2^-8 each, and pre enters the slopes), the results once more: 4 x 2^-8 of the
+    # sums of magnitudes.  fp32: 2^-24 times the number of terms (300 tokens, 96 or 80 features)
+    unit = 4 * 2.0 ** -8 if dtype == "bf16" else 320 * 2.0 ** -24
+    mag = {"h": (pre.detach()[:, :40].abs() + 1) * (xs.abs() @ w.abs().t() + b.abs())[:, 40:] + pre.detach()[:, 40:].abs() * (xs.abs() @ w.abs().t() + b.abs())[:, :40],
+           "x": (dpre.abs() + dy.abs().repeat(1, 2)) @ w.abs(), "w": (dpre.abs() + dy.abs().repeat(1, 2)).t() @ xd.abs(),
+           "b": (dpre.abs() + dy.abs().repeat(1, 2)).sum(0)}
+    for k in want:
+        diff = (got[k].cpu().double() - want[k]).abs()
+        assert bool((diff <= unit * mag[k] + 1e-30).all()), (k, float((diff / (unit * mag[k] + 1e-30)).max()))
+
+
+def test_gated_layer_random_strategy_frozen_weights_views_and_autocast():
+    print("gated layer forms", flush=True)
+    torch.manual_seed(4)
+    layer = dnn.GatedLinear(64, 32, gamma=0.7, strategy="random", seed=5, device=DEV, dtype=torch.bfloat16)
+    x = torch.randn(40, 64, device=DEV, dtype=torch.bfloat16)
+    layer(x).sum().backward()
+    first = layer.weight.grad.clone()
+    layer.weight.grad = None
+    layer(x).sum().backward()
+    assert not torch.equal(first, layer.weight.grad)               # another subset every call
+    # frozen weights: nothing is cached, x still gets its gradient
+    layer.weight.requires_grad_(False)
+    xr = x.clone().requires_grad_(True)
+    with dnn.cache_meter() as meter:
+        layer(xr).sum().backward()
+    assert meter.layers == 0 and xr.grad is not None
+    # a transposed view and one that starts inside a buffer give what their copies give
+    layer.eval()
+    big = torch.randn(64, 41, device=DEV, dtype=torch.bfloat16)
+    with torch.no_grad():
+        assert torch.equal(layer(big.t()), layer(big.t().contiguous()))
+        odd = torch.randn(64 * 9 + 3, device=DEV, dtype=torch.bfloat16)[3:].view(9, 64)
+        assert torch.equal(layer(odd), layer(odd.clone()))
+        assert layer(x[:0]).shape == (0, 32)
+    layer.train()
+    layer.weight.requires_grad_(True)
+    layer.weight.grad = None
+    layer(x[:0]).sum().backward()
+    assert bool((layer.weight.grad == 0).all())
+    # autocast: fp32 parameters, bf16 product, fp32 gradients
+    wide = dnn.GatedLinear(64, 32, gamma=0.5, device=DEV)
+    with torch.autocast("cuda", dtype=torch.bfloat16):
+        h = wide(torch.randn(20, 64, device=DEV))
+    assert h.dtype == torch.bfloat16
+    h.float().sum().backward()
+    assert wide.weight.grad.dtype == torch.float32 and bool(wide.weight.grad.isfinite().all())
+    with pytest.raises(RuntimeError):                              # no second derivative
+        xr = x.float().requires_grad_(True)
+        (gx,) = torch.autograd.grad(wide(xr).sum(), xr, create_graph=True)
+        gx.sum().backward()
+
+
+# ---- the optimizer against torch's formula in 64 bits ----------------------------------------------
+def _net(dtype):
+    torch.manual_seed(7)
+    return torch.nn.Sequential(torch.nn.Linear(48, 96), torch.nn.GELU(), torch.nn.Linear(96, 33)).to(DEV, dtype)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_adamw_follows_the_formula_over_steps(dtype):
+    print("optim", dtype, flush=True)
+    net = _net(dtype)
+    params = list(net.parameters())
+    ref = [p.detach().double().clone().requires_grad_(True) for p in params]
+    opt = dropit.optim.AdamW(params, lr=2e-3, weight_decay=0.1, max_norm=0.5)
+    gold = torch.optim.AdamW(ref, lr=2e-3, weight_decay=0.1, foreach=False)
+    g = torch.Generator(device=DEV).manual_seed(1)
+    for t in range(6):
+        for p, r in zip(params, ref):
+            p.grad = torch.randn(p.shape, generator=g, device=DEV).to(dtype)
+            r.grad = p.grad.double()
+        norm = math.sqrt(sum(float(r.grad.square().sum()) for r in ref))
+        for r in ref:
+            r.grad *= min(1.0, 0.5 / (norm + 1e-6))
+        opt.step()
+        gold.step()
+        assert abs(opt.last_grad_norm.item() / norm - 1) < 1e-5
+    for p, r in zip(params, ref):
+        master = p.detach().float()
+        if dtype == torch.bfloat16:
+            bits = (p.detach().view(torch.int16).int() << 16) + opt.state[p]["residual"].int()
+            master = bits.view(torch.float32)
+        # per step a rounding or two of p (2^-24 of it) and some ten of the update (lr times about one)
+        assert bool(((master.double() - r).abs() <= 6 * (2 * 2.0 ** -24 * r.abs() + 40 * 2.0 ** -24 * 2e-3)).all())
+        if dtype == torch.bfloat16:
+            assert bool(((p.double() - master.double()).abs() <= 2.0 ** -8 * master.double().abs()).all())
+
+
+def test_adamw_groups_layouts_and_late_parameters():
+    print("optim groups", flush=True)
+    torch.manual_seed(2)
+    conv = torch.nn.Conv2d(8, 16, 3).to(DEV).to(memory_format=torch.channels_last)
+    extra = torch.nn.Parameter(torch.randn(700, device=DEV))
+    flat = [p.detach().clone().contiguous().requires_grad_(True) for p in conv.parameters()] + [extra.detach().clone().requires_grad_(True)]
+    a = dropit.optim.AdamW([{"params": conv.parameters(), "state_bits": 8}, {"params": [extra], "lr": 5e-3, "weight_decay": 0.0}], lr=1e-3)
+    b = dropit.optim.AdamW([{"params": flat[:2]}, {"params": flat[2:], "lr": 5e-3, "weight_decay": 0.0}], lr=1e-3)
+    for t in range(3):
+        for p, q in zip(list(conv.parameters()) + [extra], flat):
+            p.grad = torch.randn(p.shape, device=DEV)              # contiguous, the parameter is not: brought to its layout
+            q.grad = p.grad.clone()
+        if t < 1:
+            extra.grad = flat[2].grad = None                       # joins later, with its own count
+        a.step()
+        b.step()
+    assert a.state[extra]["step"] == 2 and a.state[conv.weight]["step"] == 3
+    assert torch.equal(extra, flat[2])
+    # The first step is exact in eight bits too (states of zeros); the two after it differ by both sides' updates at most, and
+    # those by what the codes' rounding, less than an eighth of a value each step, makes of m and v.  After three steps: m off
+    # by at most (1 + 0.9 + 0.81) / 8 of the largest, v by a factor between (7 / 8)^3 and (9 / 8)^3; an update is lr times at
+    # most 1 in 32 bits and (1 + 0.34) / sqrt((7 / 8)^3) = 1.64 in eight.
+    with torch.no_grad():
+        assert float((conv.weight - flat[0]).abs().max()) <= 2 * (1 + 1.64) * 1e-3 * 1.01
+        m, v = a.moments(conv.weight)
+        assert m.shape == conv.weight.shape and m.stride() == conv.weight.stride()
+        want = b.moments(flat[0])
+        assert bool(((m.float() - want[0]).abs() <= 0.34 * want[0].abs().max()).all())
+        assert bool(((v.float() <= 1.425 * want[1]) & (v.float() >= 0.669 * want[1])).all())
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_adamw_state_survives_saving_and_loading(bits):
+    print("optim state", bits, flush=True)
+    net = _net(torch.bfloat16)
+    opt = dropit.optim.AdamW(net.parameters(), state_bits=bits)
+
+    def feed(net, seed):
+        g = torch.Generator(device=DEV).manual_seed(seed)
+        for p in net.parameters():
+            p.grad = torch.randn(p.shape, generator=g, device=DEV).bfloat16()
+
+    for t in range(3):
+        feed(net, t)
+        opt.step()
+    other = copy.deepcopy(net)
+    file = io.BytesIO()
+    torch.save(opt.state_dict(), file)
+    file.seek(0)
+    again = dropit.optim.AdamW(other.parameters(), lr=123.0, state_bits=bits)
+    again.load_state_dict(torch.load(file, weights_only=True))
+    for p, q in zip(net.parameters(), other.parameters()):
+        for k, v in opt.state[p].items():
+            w = again.state[q][k]
+            assert w == v if k == "step" else (w.dtype == v.dtype and torch.equal(w, v)), k
+    for t in range(3, 5):
+        feed(net, t)
+        feed(other, t)
+        opt.step()
+        again.step()
+    for p, q in zip(net.parameters(), other.parameters()):
+        assert torch.equal(p, q)
+
+
+# ---- all of it -------------------------------------------------------------------------------------
+def _block(gamma, dtype=torch.bfloat16):
+    torch.manual_seed(11)
+    net = block_bench.encoder(2, 64, 2, 256, 10, gated=True).to(DEV, dtype)
+    names = dnn.apply_dropit(net, gamma)
+    assert sum(n.endswith("fc1") for n in names) == 2              # the gated layers are among them
+    return net
+
+
+def _train(net, opt, x, target):
+    opt.zero_grad(set_to_none=False)
+    F.cross_entropy(net(x).float(), target).backward()
+    opt.step()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_training_steps_captured_into_a_graph_match_eager_ones(bits):
+    print("train graph", bits, flush=True)
+    x = torch.randn(4, 20, 64, device=DEV, dtype=torch.bfloat16)
+    target = torch.randint(0, 10, (4,), device=DEV)
+    eager, captured = _block(0.8), _block(0.8)
+    eo = dropit.optim.AdamW(eager.parameters(), lr=1e-3, state_bits=bits, max_norm=1.0, capturable=True)
+    co = dropit.optim.AdamW(captured.parameters(), lr=1e-3, state_bits=bits, max_norm=1.0, capturable=True)
+    # the first steps of both on a side stream: states, gradients and workspaces exist before the capture
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for _ in range(2):
+            _train(eager, eo, x, target)
+            _train(captured, co, x, target)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    for p, q in zip(eager.parameters(), captured.parameters()):
+        assert torch.equal(p, q)                                   # the same bits run to run
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        _train(captured, co, x, target)
+    for t in range(3):
+        fresh = torch.randn(4, 20, 64, device=DEV, dtype=torch.bfloat16)
+        x.copy_(fresh)
+        graph.replay()
+        torch.cuda.synchronize()
+        _train(eager, eo, x, target)
+        torch.cuda.synchronize()
+        for (name, p), q in zip(eager.named_parameters(), captured.parameters()):
+            # (the library's own reductions may order their sums otherwise in a graph: a rounding of a gradient, which moves
+            # a parameter by at most a few lr)
+            assert float((p.detach().float() - q.detach().float()).abs().max()) <= 4e-3 * (t + 1), name
+    assert int(next(iter(co.state.values()))["step"]) == int(next(iter(eo.state.values()))["step"]) == 5
+
+
+def test_capture_is_refused_where_a_replay_would_be_wrong():
+    print("optim capture refusals", flush=True)
+    p = torch.nn.Parameter(torch.zeros(300, device=DEV))
+    p.grad = torch.ones(300, device=DEV)
+    plain, late = dropit.optim.AdamW([p]), dropit.optim.AdamW([p], capturable=True)
+    plain.step()
+    for opt, words in ((plain, "capturable=True"), (late, "outside the capture")):
+        graph = torch.cuda.CUDAGraph()
+        spare = torch.zeros(1, device=DEV)
+        with torch.cuda.graph(graph):
+            spare.add_(1)
+            with pytest.raises(RuntimeError, match=words):
+                opt.step()
+    q = torch.nn.Parameter(torch.zeros(3, device=DEV))
+    both = dropit.optim.AdamW([p, q], capturable=True)
+    with pytest.raises(RuntimeError, match="no gradient"):
+        both.step()
+
+
+def test_block_bench_runs_with_the_gated_block_and_adamw():
+    print("block bench", flush=True)
+    import argparse
+    for mlp, optimizer in (("gated", "adamw8"), ("gated", "adamw"), ("gelu", "sgd")):
+        args = argparse.Namespace(batch=2, tokens=17, dim=64, heads=2, depth=3, steps=2, warmup=1, index="flat", mlp=mlp, optimizer=optimizer)
+        out = block_bench.run(0.9, args)
+        assert out["dropit_layers"] == 12 and out["ms_per_iter"] > 0 and out["value_cache_GiB"] >= 0

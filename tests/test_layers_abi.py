@@ -116,11 +116,11 @@ def test_gated_projection_refuses_bad_arguments_without_a_gpu():
                dict(t=1 << 31), dict(t=(1 << 31) - 1, n=1 << 20), dict(dt=2), dict(act=-1), dict(act=5)):
         assert forward(**kw) == binding.EINVAL, kw
     assert forward(t=0, x=None, w=None, h=None) == binding.OK
-    need = L.dropit_gated_forward_workspace_bytes(1, 4096, 64, binding.F32)
+    need = L.dropit_gated_forward_workspace_bytes(1, 4097, 64, binding.F32)          # (odd rows, few tiles: in slices)
     assert need > 0
-    assert forward(t=1, c=4096, n=64, dt=binding.F32, nbytes=need - 1) == binding.EWORKSPACE
-    assert forward(t=1, c=4096, n=64, dt=binding.F32, ws=None) == binding.EINVAL
-    assert forward(t=1, c=4096, n=64, dt=binding.F32, ws=FAKE + 16) == binding.EINVAL
+    assert forward(t=1, c=4097, n=64, dt=binding.F32, nbytes=need - 1) == binding.EWORKSPACE
+    assert forward(t=1, c=4097, n=64, dt=binding.F32, ws=None) == binding.EINVAL
+    assert forward(t=1, c=4097, n=64, dt=binding.F32, ws=FAKE + 16) == binding.EINVAL
 
     def backward(dh=FAKE, pre=FAKE, t=10, c=16, dt=binding.BF16, w=FAKE, n=8, act=0, dpre=FAKE, dx=FAKE, db=FAKE, ws=FAKE, nbytes=big):
         return L.dropit_gated_backward(dh, pre, t, c, dt, w, n, act, dpre, dx, db, ws, nbytes, None)
@@ -131,7 +131,7 @@ def test_gated_projection_refuses_bad_arguments_without_a_gpu():
         assert backward(**kw) == binding.EINVAL, kw
     assert backward(nbytes=16) == binding.EWORKSPACE
     assert L.dropit_gated_backward_workspace_bytes(10, 16, 8, binding.BF16, 0, 0) == 0
-    assert L.dropit_gated_backward_workspace_bytes(10, 16, 8, binding.BF16, 0, 1) == 16 * 4
+    assert L.dropit_gated_backward_workspace_bytes(10, 16, 8, binding.BF16, 0, 1) == 3 * 16 * 4       # blocks of four tokens
     assert L.dropit_gated_backward_workspace_bytes(10, 0, 8, binding.BF16, 1, 1) == 0
 
 

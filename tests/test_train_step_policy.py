@@ -1,0 +1,65 @@
+"""What nn.GatedLinear and optim.AdamW do without a GPU: plain inference and baseline training, the layer policy, refusals."""
+import pytest
+import torch
+import torch.nn.functional as F
+
+import paper_2202_13808_amd as dropit
+from paper_2202_13808_amd import nn as dnn
+
+
+@pytest.mark.parametrize("act,fn", [("silu", F.silu), ("gelu", F.gelu), ("gelu_tanh", lambda z: F.gelu(z, approximate="tanh")),
+                                    ("relu", F.relu), ("sigmoid", torch.sigmoid)])
+def test_gated_linear_on_the_host_is_the_plain_layer(act, fn):
+    torch.manual_seed(1)
+    layer = dnn.GatedLinear(12, 10, act=act, gamma=0.0)
+    x = torch.randn(3, 5, 12, requires_grad=True)
+    want = fn(F.linear(x, layer.weight[:10], layer.bias[:10])) * F.linear(x, layer.weight[10:], layer.bias[10:])
+    assert torch.allclose(layer(x), want, atol=1e-6)
+    layer(x).sum().backward()
+    assert layer.weight.grad.shape == (20, 12) and layer.bias.grad.shape == (20,) and x.grad.shape == x.shape
+    with torch.no_grad():
+        assert torch.allclose(dnn.GatedLinear.forward(layer.eval(), x), want, atol=1e-6)
+
+
+def test_gated_linear_drops_on_device_tensors_only():
+    layer = dnn.GatedLinear(8, 4)
+    with pytest.raises(RuntimeError, match="no CPU path"):
+        layer(torch.randn(2, 8))
+    layer.eval()
+    assert layer(torch.randn(2, 8)).shape == (2, 4)
+
+
+def test_gated_linear_refuses_bad_arguments():
+    for kw in (dict(act="tanh"), dict(strategy="top"), dict(index_format="csr"), dict(strategy="random", index_format="rows")):
+        with pytest.raises(ValueError):
+            dnn.GatedLinear(8, 4, **kw)
+    with pytest.raises(ValueError):
+        dnn.gated_linear(torch.randn(2, 8), torch.randn(7, 8))
+    with pytest.raises(ValueError):
+        dnn.gated_linear(torch.randn(2, 8), torch.randn(6, 8), act="swish")
+
+
+def test_apply_dropit_sets_the_rate_of_gated_layers_too():
+    net = torch.nn.Sequential(torch.nn.Linear(8, 8), dnn.GatedLinear(8, 6, gamma=0.0), torch.nn.Linear(6, 8), torch.nn.Linear(8, 2))
+    keys = list(net.state_dict())
+    assert dropit.nn.apply_dropit(net, 0.8, index_format="mask") == ["1", "2"]
+    assert net[1].gamma == 0.8 and net[1].index_format == "mask" and type(net[1]) is dnn.GatedLinear
+    assert list(net.state_dict()) == keys
+
+
+def test_adamw_refuses_bad_arguments():
+    p = torch.nn.Parameter(torch.zeros(4))
+    for kw in (dict(lr=-1.0), dict(betas=(1.0, 0.9)), dict(betas=(0.9, -0.1)), dict(eps=-1e-8), dict(weight_decay=-0.1),
+               dict(state_bits=16), dict(max_norm=0.0), dict(lr=float("nan"))):
+        with pytest.raises(ValueError):
+            dropit.optim.AdamW([p], **kw)
+    with pytest.raises(TypeError):
+        dropit.optim.AdamW([p], lr=torch.tensor(1e-3))
+    for bad in (torch.zeros(4, dtype=torch.float16), torch.zeros(4, dtype=torch.float64), torch.zeros(8)[::2], torch.zeros(4, 1).expand(4, 3)):
+        with pytest.raises(TypeError):
+            dropit.optim.AdamW([torch.nn.Parameter(bad)])
+    opt = dropit.optim.AdamW([p])
+    opt.step()                                         # no gradients: nothing to do
+    p.grad = torch.ones(4)
+    with pytest.raises(RuntimeError, match="no CPU path"):
+        opt.step()
