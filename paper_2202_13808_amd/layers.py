@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import math
-from array import array
+import struct
 from operator import attrgetter
 from typing import List, Optional, Sequence, Tuple, Union
 
@@ -150,12 +150,16 @@ def _one_dtype(tensors: Sequence[torch.Tensor], allowed, what: str) -> torch.dty
     return found.pop()
 
 
-def _pointers(tensors: Sequence[torch.Tensor]) -> array:
-    return array("q", map(torch.Tensor.data_ptr, tensors))
+def _pointers(tensors: Sequence[torch.Tensor]) -> List[int]:
+    return list(map(torch.Tensor.data_ptr, tensors))
 
 
-def _numels(tensors: Sequence[torch.Tensor]) -> array:
-    return array("q", map(torch.Tensor.numel, tensors))
+def _numels(tensors: Sequence[torch.Tensor]) -> List[int]:
+    return list(map(torch.Tensor.numel, tensors))
+
+
+def _int64(values: List[int]) -> np.ndarray:
+    return np.frombuffer(struct.pack("%dq" % len(values), *values), dtype=np.int64)      # (np.array asks each value what it is)
 
 
 def _scalar(t: Optional[torch.Tensor], dtype: torch.dtype, device: int, what: str) -> Optional[int]:
@@ -203,24 +207,23 @@ def adamw(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], m: Sequ
         if _numels(x) != numels:
             raise ValueError("%s must have as many elements as their parameters" % name)
     table = np.zeros((count, 8), dtype=np.int64)
-    column = lambda x: np.frombuffer(x, dtype=np.int64)  # noqa: E731
     if bits8:
-        blocks = (column(numels) + (ADAMW_BLOCK - 1)) // ADAMW_BLOCK
+        blocks = (_int64(numels) + (ADAMW_BLOCK - 1)) // ADAMW_BLOCK
         for at, x in ((4, m_offset), (5, v_offset)):
             _one_dtype(x, (torch.int16,), "offsets of 8-bit states")
-            if bool((column(_numels(x)) < blocks).any()):
+            if bool((_int64(_numels(x)) < blocks).any()):
                 raise ValueError("an offset for every %d elements of a parameter" % ADAMW_BLOCK)
-            table[:, at] = column(_pointers(x))
+            table[:, at] = _int64(_pointers(x))
     if residual is not None:
         if p_dtype != torch.bfloat16:
             raise TypeError("residuals belong to bfloat16 parameters")
         _one_dtype(residual, (torch.int16,), "residuals")
-        table[:, 6] = column(_pointers(residual))
+        table[:, 6] = _int64(_pointers(residual))
     pointers = _pointers(params)
     if len(set(pointers)) != count and len({q for q, n in zip(pointers, numels) if n}) != sum(1 for n in numels if n):
         raise ValueError("a parameter appears twice in one step")
     for at, x in ((0, pointers), (1, _pointers(grads)), (2, _pointers(m)), (3, _pointers(v)), (7, numels)):
-        table[:, at] = column(x)
+        table[:, at] = _int64(x)
     hyper = _AdamwHyper(float(lr), float(betas[0]), float(betas[1]), float(eps), float(weight_decay), step_host,
                         _scalar(step, torch.int32, device, "step") if isinstance(step, torch.Tensor) else None,
                         _scalar(grad_scale, torch.float32, device, "grad_scale"))
@@ -272,8 +275,8 @@ def grad_norm(grads: Sequence[torch.Tensor], max_norm: float = math.inf, out: Op
         out = torch.empty(2, dtype=torch.float32, device=where)
     elif out.dtype != torch.float32 or out.numel() < 2 or out.get_device() != device or not out.is_contiguous():
         raise ValueError("out must hold two contiguous float32 elements on the gradients' device")
-    pointers, numels = _pointers(grads), _numels(grads)
-    at_pointers, at_numels = pointers.buffer_info()[0], numels.buffer_info()[0]
+    pointers, numels = _int64(_pointers(grads)), _int64(_numels(grads))
+    at_pointers, at_numels = pointers.ctypes.data, numels.ctypes.data
     need = int(lib().dropit_grad_norm_workspace_bytes(at_numels, count))
     if workspace is None:
         workspace = torch.empty(need, dtype=torch.uint8, device=where) if need else None
