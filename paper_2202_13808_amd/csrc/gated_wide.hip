@@ -44,6 +44,7 @@ namespace {
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+typedef u32x4 u32x4_any __attribute__((aligned(2)));       // at any element's address
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(16))) float f32x16;
@@ -359,8 +360,8 @@ gated_wide_kernel(const WideArgs a)
                 }
                 const int c = n + (q + half) * 8;
                 if (t >= a.tokens || c >= width) continue;
-                if (width % 8 == 0) {                  // (then every row starts on 16 bytes)
-                    *reinterpret_cast<u32x4 *>(to + c) = w;
+                if (c + 8 <= width) {
+                    *reinterpret_cast<u32x4_any *>(to + c) = w;
                 } else {
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
