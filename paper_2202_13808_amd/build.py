@@ -1,14 +1,16 @@
-"""Builds the gfx950 shared library ``libdropit.so`` in-tree with hipcc."""
+"""Builds the gfx950 shared library ``libdropit.so`` in-tree with hipcc, and the Python module that reads tensors for it."""
 from __future__ import annotations
 
 import glob
 import os
 import subprocess
+import sysconfig
 
 PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG_DIR, "csrc")
 INCLUDE = os.path.join(os.path.dirname(PKG_DIR), "include")
 LIB_PATH = os.path.join(PKG_DIR, "libdropit.so")
+MARSHAL_PATH = os.path.join(PKG_DIR, "_marshal.so")
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
@@ -22,8 +24,28 @@ def sources():
     return sorted(glob.glob(os.path.join(CSRC, "*.hip")))
 
 
+def build_marshal(verbose: bool = False) -> str:
+    """Compile the module that asks many tensors for their addresses in one call (host code only)."""
+    import torch
+    from torch.utils import cpp_extension
+    libs = os.path.join(os.path.dirname(torch.__file__), "lib")
+    tmp = MARSHAL_PATH + ".tmp.%d" % os.getpid()
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-Wall",
+           "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI), "-I", sysconfig.get_paths()["include"]]
+    for path in cpp_extension.include_paths():
+        cmd += ["-isystem", path]
+    cmd += ["-o", tmp, os.path.join(CSRC, "marshal.cpp"), "-L", libs, "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10",
+            "-Wl,-rpath," + libs]
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    subprocess.check_call(cmd)
+    os.replace(tmp, MARSHAL_PATH)
+    return MARSHAL_PATH
+
+
 def build(verbose: bool = False) -> str:
-    """Compile every HIP source for gfx950 into one shared library; returns its path."""
+    """Compile every HIP source for gfx950 into one shared library, and the marshalling module; returns the library's path."""
+    build_marshal(verbose)
     tmp = LIB_PATH + ".tmp.%d" % os.getpid()
     cmd = [HIPCC] + FLAGS + ["-I", INCLUDE, "-I", CSRC, "-o", tmp] + sources()
     if verbose:

@@ -2,8 +2,8 @@
 //
 // A streaming operator: 28 bytes an element with everything in fp32, 10 in bf16 with 8-bit states.  What it must not do
 // is start a kernel per tensor or keep a table of pointers in device memory that gradients allocated anew each step
-// would outdate: the table of up to MAX_TENSORS tensors travels in the kernel's arguments, and a workgroup finds its tensor
-// by a search over the tensors' first chunks.
+// would outdate: the table of 58 to 90 tensors, by how many pointers each needs, travels in the kernel's arguments, and a
+// workgroup finds its tensor by a search over the tensors' first chunks.
 //
 // A thread takes 8 consecutive elements, so that bf16 moves 16 bytes an access and 8-bit codes 8; 32 lanes share a block of
 // 256 elements and find its largest pattern by five lane exchanges, without LDS or a second pass over the data.
@@ -11,6 +11,7 @@
 // The arithmetic is that of single fp32 operations, correctly rounded division and square root included: the codes and the
 // residual's 16 bits are exact functions of the inputs, which any other implementation of the formulas reproduces.
 #include <cmath>
+#include <type_traits>
 
 #include "common.hpp"
 #include "dropit_layers.h"
@@ -22,7 +23,6 @@ constexpr int ADAMW_THREADS = 256;
 constexpr int ADAMW_PER_THREAD = 8;
 constexpr int ADAMW_ROUNDS = 2;                                             // rounds of 2048 elements a workgroup makes
 constexpr int ADAMW_CHUNK = ADAMW_THREADS * ADAMW_PER_THREAD * ADAMW_ROUNDS;
-constexpr int MAX_TENSORS = 48;                                             // 48 x 68 bytes: arguments stay under 4 KB
 constexpr uint32_t WEYL_I = 0x6a09e667u, WEYL_T = 0x9e3779b9u;              // odd: every residue mod 2^32 once a period
 constexpr uint32_t LAST_FINITE = 0x7f7u, NAN_OFFSET = 0x7f9u, NAN_CODE = 0x7ffu;
 
@@ -30,9 +30,14 @@ constexpr int64_t ADAMW_MAX_NUMEL = int64_t(1) << 34;                       // a
 constexpr uint32_t MAX_CHUNKS = 1u << 23;
 static_assert(ADAMW_MAX_NUMEL / ADAMW_CHUNK <= MAX_CHUNKS && ADAMW_MAX_NUMEL / (ADAMW_THREADS * ADAMW_PER_THREAD) <= MAX_CHUNKS, "");
 
-struct AdamwTable {
-    dropit_adamw_tensor t[MAX_TENSORS];
-    uint32_t first[MAX_TENSORS];                       // first chunk of each tensor
+// p, g, m, v, then the offsets of 8-bit states, then the residual: what a kind of step needs of each tensor.  As many tensors as
+// keep the arguments under 4 KB (48 of them took 4 launches for the 152 tensors of a 12-block encoder, 147 us for 140)
+template <bool RESIDUAL, bool BITS8> struct AdamwTable {
+    static constexpr int POINTERS = 4 + (BITS8 ? 2 : 0) + (RESIDUAL ? 1 : 0);
+    static constexpr int MOST = (4096 - 128) / (POINTERS * 8 + 12);
+    void *pointer[POINTERS][MOST];
+    int64_t numel[MOST];
+    uint32_t first[MOST];                              // first chunk of each tensor
     int count;
 };
 
@@ -44,7 +49,7 @@ struct AdamwScalars {
     const int32_t *step;                               // device step, or null
     double lr, beta1d, beta2d;
 };
-static_assert(sizeof(AdamwTable) + sizeof(AdamwScalars) <= 4096, "kernel arguments");
+static_assert(sizeof(AdamwScalars) <= 112, "kernel arguments");
 
 typedef __attribute__((ext_vector_type(4))) float af32x4;
 typedef __attribute__((ext_vector_type(4))) uint32_t au32x4;
@@ -320,7 +325,7 @@ __device__ inline void adamw_elements(const dropit_adamw_tensor &t, const AdamwS
 
 template <bool P_BF16, bool RESIDUAL, bool G_BF16, bool BITS8>
 __global__ void __launch_bounds__(ADAMW_THREADS)
-adamw_kernel(const AdamwTable table, const AdamwScalars s)
+adamw_kernel(const AdamwTable<RESIDUAL, BITS8> table, const AdamwScalars s)
 {
     __shared__ float shared[2];
     // the last tensor whose first chunk is not behind this one
@@ -329,7 +334,17 @@ adamw_kernel(const AdamwTable table, const AdamwScalars s)
         const int mid = (lo + hi + 1) >> 1;
         if (table.first[mid] <= blockIdx.x) lo = mid; else hi = mid - 1;
     }
-    const dropit_adamw_tensor t = table.t[lo];
+    dropit_adamw_tensor t = {};
+    t.p = table.pointer[0][lo];
+    t.g = table.pointer[1][lo];
+    t.m = table.pointer[2][lo];
+    t.v = table.pointer[3][lo];
+    if constexpr (BITS8) {
+        t.m_offset = static_cast<int16_t *>(table.pointer[4][lo]);
+        t.v_offset = static_cast<int16_t *>(table.pointer[5][lo]);
+    }
+    if constexpr (RESIDUAL) t.residual = static_cast<int16_t *>(table.pointer[table.POINTERS - 1][lo]);
+    t.numel = table.numel[lo];
     float root2 = s.root2, rate = s.rate;
     uint32_t weyl_t = s.weyl;
     if (s.step != nullptr) {
@@ -381,11 +396,40 @@ adamw_unpack_kernel(const uint8_t *__restrict__ codes, const int16_t *__restrict
     store8_u16<false>(values, i, n, wide, out);
 }
 
-template <bool P_BF16, bool RESIDUAL, bool G_BF16>
-void launch_adamw(bool bits8, const AdamwTable &table, const AdamwScalars &s, uint32_t chunks, hipStream_t stream)
+template <bool P_BF16, bool RESIDUAL, bool G_BF16, bool BITS8>
+void launch_adamw(const dropit_adamw_tensor *tensors, int64_t count, const AdamwScalars &s, hipStream_t stream)
 {
-    if (bits8) adamw_kernel<P_BF16, RESIDUAL, G_BF16, true><<<chunks, ADAMW_THREADS, 0, stream>>>(table, s);
-    else adamw_kernel<P_BF16, RESIDUAL, G_BF16, false><<<chunks, ADAMW_THREADS, 0, stream>>>(table, s);
+    using Table = AdamwTable<RESIDUAL, BITS8>;
+    static_assert(sizeof(Table) + sizeof(AdamwScalars) <= 4096, "kernel arguments");
+    Table table;
+    table.count = 0;
+    uint32_t chunks = 0;
+    auto flush = [&]() {
+        if (table.count == 0) return;
+        adamw_kernel<P_BF16, RESIDUAL, G_BF16, BITS8><<<chunks, ADAMW_THREADS, 0, stream>>>(table, s);
+        table.count = 0;
+        chunks = 0;
+    };
+    for (int64_t j = 0; j < count; ++j) {
+        const dropit_adamw_tensor &t = tensors[j];
+        if (t.numel == 0) continue;
+        const uint32_t need = uint32_t((t.numel + ADAMW_CHUNK - 1) / ADAMW_CHUNK);
+        if (table.count == Table::MOST || chunks + need > MAX_CHUNKS) flush();
+        const int at = table.count++;
+        table.pointer[0][at] = t.p;
+        table.pointer[1][at] = const_cast<void *>(t.g);
+        table.pointer[2][at] = t.m;
+        table.pointer[3][at] = t.v;
+        if constexpr (BITS8) {
+            table.pointer[4][at] = t.m_offset;
+            table.pointer[5][at] = t.v_offset;
+        }
+        if constexpr (RESIDUAL) table.pointer[Table::POINTERS - 1][at] = t.residual;
+        table.numel[at] = t.numel;
+        table.first[at] = chunks;
+        chunks += need;
+    }
+    flush();
 }
 
 bool valid_dtype(dropit_dtype dt) { return dt == DROPIT_F32 || dt == DROPIT_BF16; }
@@ -446,34 +490,16 @@ extern "C" dropit_status dropit_adamw(const dropit_adamw_tensor *tensors, int64_
     s.beta1d = h.beta1;
     s.beta2d = h.beta2;
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    AdamwTable table;
-    table.count = 0;
-    uint32_t chunks = 0;
-    auto flush = [&]() {
-        if (table.count == 0) return;
-        if (!pbf) {
-            if (gbf) launch_adamw<false, false, true>(bits8, table, s, chunks, stream);
-            else launch_adamw<false, false, false>(bits8, table, s, chunks, stream);
-        } else if (residual) {
-            if (gbf) launch_adamw<true, true, true>(bits8, table, s, chunks, stream);
-            else launch_adamw<true, true, false>(bits8, table, s, chunks, stream);
-        } else {
-            if (gbf) launch_adamw<true, false, true>(bits8, table, s, chunks, stream);
-            else launch_adamw<true, false, false>(bits8, table, s, chunks, stream);
-        }
-        table.count = 0;
-        chunks = 0;
+    auto launch = [&](auto p, auto r, auto g) {
+        constexpr bool P = decltype(p)::value, R = decltype(r)::value, G = decltype(g)::value;
+        if (bits8) launch_adamw<P, R, G, true>(tensors, count, s, stream);
+        else launch_adamw<P, R, G, false>(tensors, count, s, stream);
     };
-    for (int64_t j = 0; j < count; ++j) {
-        if (tensors[j].numel == 0) continue;
-        const uint32_t need = uint32_t((tensors[j].numel + ADAMW_CHUNK - 1) / ADAMW_CHUNK);
-        if (table.count == MAX_TENSORS || chunks + need > MAX_CHUNKS) flush();
-        table.t[table.count] = tensors[j];
-        table.first[table.count] = chunks;
-        ++table.count;
-        chunks += need;
-    }
-    flush();
+    constexpr std::true_type yes{};
+    constexpr std::false_type no{};
+    if (!pbf) gbf ? launch(no, no, yes) : launch(no, no, no);
+    else if (residual) gbf ? launch(yes, yes, yes) : launch(yes, yes, no);
+    else gbf ? launch(yes, no, yes) : launch(yes, no, no);
     return launch_status();
 }
 

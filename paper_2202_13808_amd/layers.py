@@ -8,9 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import math
-import struct
-from operator import attrgetter
-from typing import List, Optional, Sequence, Tuple, Union
+from typing import NamedTuple, Optional, Sequence, Tuple, Union
 
 import numpy as np
 import torch
@@ -19,7 +17,7 @@ from .binding import BF16, F32, _check, _dtype_code, _on, _require_device, _stre
 
 ADAMW_BLOCK = 256      # DROPIT_ADAMW_BLOCK: elements that share an offset of the 8-bit states
 
-_CODES = {torch.float32: F32, torch.bfloat16: BF16}
+_UINT8, _INT16 = 2, 3  # csrc/marshal.cpp's codes beside F32 and BF16
 
 
 ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "relu": 3, "sigmoid": 4}      # dropit_act
@@ -127,39 +125,45 @@ class _AdamwHyper(ctypes.Structure):
         ("step", ctypes.c_int64), ("step_device", ctypes.c_void_p), ("grad_scale", ctypes.c_void_p)]
 
 
-# What a call over hundreds of tensors asks of each goes through map() over the tensor's own methods, some 40 ns a tensor and
-# question; a step of 152 tensors asks twenty, and the kernels of a small encoder take 140 us.
-_dtype_of = attrgetter("dtype")
+_TYPES = (torch.float32, torch.bfloat16, torch.uint8, torch.int16)      # by the codes of csrc/marshal.cpp
+_marshal_module = None
 
 
-def _same_device(*lists: Sequence[torch.Tensor]) -> int:
-    found = set()
-    for tensors in lists:
-        found.update(map(torch.Tensor.get_device, tensors))
-        if not all(map(torch.Tensor.is_contiguous, tensors)):
-            raise ValueError("dropit tensors must be contiguous")
-    if len(found) != 1 or -1 in found:
-        raise ValueError("dropit operates on device tensors only (no CPU path), and on one device per call")
-    return found.pop()
+def _marshal():
+    """The module that reads many tensors in one call.  Raises if it has not been built (no fallback)."""
+    global _marshal_module
+    if _marshal_module is None:
+        try:
+            from . import _marshal as module
+        except ImportError as e:
+            raise ImportError("_marshal.so is missing: build it with `python -m paper_2202_13808_amd.build`") from e
+        _marshal_module = module
+    return _marshal_module
 
 
-def _one_dtype(tensors: Sequence[torch.Tensor], allowed, what: str) -> torch.dtype:
-    found = set(map(_dtype_of, tensors))
-    if len(found) != 1 or not found <= set(allowed):
-        raise TypeError("%s must all be %s, got %s" % (what, " or ".join(map(str, allowed)), sorted(map(str, found))))
-    return found.pop()
+class _Tensors(NamedTuple):
+    """What a call asks of a list of tensors: addresses and sizes, the types one by one, the one type and device of all."""
+    pointers: bytes
+    numels: bytes
+    types: bytes
+    type: int
+    device: int
+    contiguous: bool
 
 
-def _pointers(tensors: Sequence[torch.Tensor]) -> List[int]:
-    return list(map(torch.Tensor.data_ptr, tensors))
+def _read(tensors: Sequence[torch.Tensor], what: str, allowed: Tuple[int, ...]) -> _Tensors:
+    found = _Tensors(*_marshal().describe(tensors))
+    if found.device < 0:
+        raise ValueError("dropit operates on device tensors only (no CPU path), and on one device per call: %s" % what)
+    if not found.contiguous:
+        raise ValueError("dropit tensors must be contiguous: %s" % what)
+    if found.type not in allowed:
+        raise TypeError("%s must all be %s, got %s" % (what, " or ".join(str(_TYPES[c]) for c in allowed if c >= 0), sorted({str(t.dtype) for t in tensors})))
+    return found
 
 
-def _numels(tensors: Sequence[torch.Tensor]) -> List[int]:
-    return list(map(torch.Tensor.numel, tensors))
-
-
-def _int64(values: List[int]) -> np.ndarray:
-    return np.frombuffer(struct.pack("%dq" % len(values), *values), dtype=np.int64)      # (np.array asks each value what it is)
+def _int64(raw: bytes) -> np.ndarray:
+    return np.frombuffer(raw, dtype=np.int64)
 
 
 def _scalar(t: Optional[torch.Tensor], dtype: torch.dtype, device: int, what: str) -> Optional[int]:
@@ -196,40 +200,39 @@ def adamw(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], m: Sequ
             raise ValueError("step counts from 1, got %d" % step_host)
     if count == 0:
         return
-    device = _same_device(*lists)
-    p_dtype = _one_dtype(params, (torch.float32, torch.bfloat16), "parameters")
-    g_dtype = _one_dtype(grads, (torch.float32, torch.bfloat16), "gradients")
-    state_dtype = (torch.uint8,) if bits8 else (torch.float32,)
-    _one_dtype(m, state_dtype, "states m")
-    _one_dtype(v, state_dtype, "states v")
-    numels = _numels(params)
-    for name, x in (("gradients", grads), ("m", m), ("v", v)) + ((("residual", residual),) if residual is not None else ()):
-        if _numels(x) != numels:
-            raise ValueError("%s must have as many elements as their parameters" % name)
-    table = np.zeros((count, 8), dtype=np.int64)
-    if bits8:
-        blocks = (_int64(numels) + (ADAMW_BLOCK - 1)) // ADAMW_BLOCK
-        for at, x in ((4, m_offset), (5, v_offset)):
-            _one_dtype(x, (torch.int16,), "offsets of 8-bit states")
-            if bool((_int64(_numels(x)) < blocks).any()):
-                raise ValueError("an offset for every %d elements of a parameter" % ADAMW_BLOCK)
-            table[:, at] = _int64(_pointers(x))
+    p = _read(params, "parameters", (F32, BF16))
+    state_type = (_UINT8,) if bits8 else (F32,)
+    columns = [(1, "gradients", _read(grads, "gradients", (F32, BF16))), (2, "m", _read(m, "states m", state_type)),
+               (3, "v", _read(v, "states v", state_type))]
     if residual is not None:
-        if p_dtype != torch.bfloat16:
+        if p.type != BF16:
             raise TypeError("residuals belong to bfloat16 parameters")
-        _one_dtype(residual, (torch.int16,), "residuals")
-        table[:, 6] = _int64(_pointers(residual))
-    pointers = _pointers(params)
-    if len(set(pointers)) != count and len({q for q, n in zip(pointers, numels) if n}) != sum(1 for n in numels if n):
-        raise ValueError("a parameter appears twice in one step")
-    for at, x in ((0, pointers), (1, _pointers(grads)), (2, _pointers(m)), (3, _pointers(v)), (7, numels)):
-        table[:, at] = _int64(x)
+        columns.append((6, "residuals", _read(residual, "residuals", (_INT16,))))
+    table = np.zeros((count, 8), dtype=np.int64)
+    for at, what, x in columns:
+        if x.numels != p.numels:
+            raise ValueError("%s must have as many elements as their parameters" % what)
+        if x.device != p.device:
+            raise ValueError("%s must be on their parameters' device" % what)
+        table[:, at] = _int64(x.pointers)
+    numels, pointers = _int64(p.numels), _int64(p.pointers)
+    if bits8:
+        for at, x in ((4, _read(m_offset, "offsets of 8-bit states", (_INT16,))), (5, _read(v_offset, "offsets of 8-bit states", (_INT16,)))):
+            if x.device != p.device or bool((_int64(x.numels) < (numels + (ADAMW_BLOCK - 1)) // ADAMW_BLOCK).any()):
+                raise ValueError("an offset for every %d elements of a parameter, on its device" % ADAMW_BLOCK)
+            table[:, at] = _int64(x.pointers)
+    if len(set(pointers.tolist())) != count:
+        real = pointers[numels > 0].tolist()
+        if len(set(real)) != len(real):
+            raise ValueError("a parameter appears twice in one step")
+    table[:, 0], table[:, 7] = pointers, numels
+    device = p.device
     hyper = _AdamwHyper(float(lr), float(betas[0]), float(betas[1]), float(eps), float(weight_decay), step_host,
                         _scalar(step, torch.int32, device, "step") if isinstance(step, torch.Tensor) else None,
                         _scalar(grad_scale, torch.float32, device, "grad_scale"))
     where = params[0].device
     with _on(where):
-        _check(lib().dropit_adamw(table.ctypes.data, count, _CODES[p_dtype], _CODES[g_dtype], 8 if bits8 else 32,
+        _check(lib().dropit_adamw(table.ctypes.data, count, p.type, columns[0][2].type, 8 if bits8 else 32,
                                   ctypes.byref(hyper), _stream_ptr(stream, where)))
 
 
@@ -262,20 +265,16 @@ def grad_norm(grads: Sequence[torch.Tensor], max_norm: float = math.inf, out: Op
         raise ValueError("max_norm must be positive, got %r" % (max_norm,))
     if count == 0:
         raise ValueError("grad_norm needs a tensor (it tells the device)")
-    device = _same_device(grads)
-    types = set(map(_dtype_of, grads))
-    if not types <= set(_CODES):
-        raise TypeError("dropit supports float32 and bfloat16 tensors, got %s" % sorted(map(str, types)))
-    if len(types) == 1:
-        dtypes = np.full(count, _CODES[types.pop()], dtype=np.int32)
-    else:
-        dtypes = np.array([_CODES[t.dtype] for t in grads], dtype=np.int32)
+    g = _read(grads, "gradients", (F32, BF16, -2))
+    device, dtypes = g.device, np.frombuffer(g.types, dtype=np.int32)
+    if g.type == -2 and not bool(((dtypes == F32) | (dtypes == BF16)).all()):
+        raise TypeError("dropit supports float32 and bfloat16 tensors, got %s" % sorted({str(t.dtype) for t in grads}))
     where = grads[0].device
     if out is None:
         out = torch.empty(2, dtype=torch.float32, device=where)
     elif out.dtype != torch.float32 or out.numel() < 2 or out.get_device() != device or not out.is_contiguous():
         raise ValueError("out must hold two contiguous float32 elements on the gradients' device")
-    pointers, numels = _int64(_pointers(grads)), _int64(_numels(grads))
+    pointers, numels = _int64(g.pointers), _int64(g.numels)
     at_pointers, at_numels = pointers.ctypes.data, numels.ctypes.data
     need = int(lib().dropit_grad_norm_workspace_bytes(at_numels, count))
     if workspace is None:

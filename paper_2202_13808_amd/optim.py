@@ -27,8 +27,12 @@ def _memory_order(t: torch.Tensor) -> torch.Tensor:
     return v
 
 
+def _contiguous(tensors: List[torch.Tensor]) -> bool:
+    return layers._marshal().describe(tensors)[5]
+
+
 def _all_in_memory_order(tensors: List[torch.Tensor]) -> List[torch.Tensor]:
-    return tensors if all(map(torch.Tensor.is_contiguous, tensors)) else [_memory_order(t) for t in tensors]
+    return tensors if _contiguous(tensors) else [_memory_order(t) for t in tensors]
 
 
 class AdamW(torch.optim.Optimizer):
@@ -133,9 +137,9 @@ class AdamW(torch.optim.Optimizer):
             if not params:
                 continue
             grads = [g for _, g in pairs if g is not None]
-            if min(map(torch.Tensor.get_device, params)) < 0:
+            if layers._marshal().describe(params)[4] == -1:
                 raise RuntimeError("AdamW steps device parameters only: there is no CPU path")
-            if not (all(map(torch.Tensor.is_contiguous, params)) and all(map(torch.Tensor.is_contiguous, grads))):
+            if not (_contiguous(params) and _contiguous(grads)):
                 grads = [self._grad(p, g) for p, g in zip(params, grads)]
             states = [self.state[p] for p in params]
             if group["capturable"]:
