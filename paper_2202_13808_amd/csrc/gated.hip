@@ -292,25 +292,86 @@ dropit_status launch_generic(GenArgs a, hipStream_t stream)
     return launch_status();
 }
 
-// bf16 on wide tiles
-template <bool FORWARD>
-dropit_status launch_wide(GenArgs a, const WidePlan &plan, hipStream_t stream)
+// Rows of any length into rows of whole 16-byte units, zeros behind the end.
+__global__ void __launch_bounds__(256)
+gated_pad_kernel(const void *__restrict__ from, int64_t rows, int length, int pitch, uint16_t *__restrict__ to)
 {
+    const int units = pitch / 8;
+    const int64_t total = rows * units;
+    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < total; i += int64_t(gridDim.x) * 256) {
+        const int64_t r = i / units;
+        const int k = int(i - r * units) * 8;
+        *reinterpret_cast<u32x4 *>(to + r * pitch + k) = load_unit<true>(from, r, length, k, length);
+    }
+}
+
+void launch_pad(const void *from, int64_t rows, int length, int pitch, void *to, hipStream_t stream)
+{
+    const int64_t blocks = (rows * (pitch / 8) + 255) / 256;
+    gated_pad_kernel<<<static_cast<uint32_t>(std::min<int64_t>(blocks, 1 << 16)), 256, 0, stream>>>(from, rows, length, pitch, static_cast<uint16_t *>(to));
+}
+
+// Whether a product runs on wide tiles, and what it keeps in the workspace: the slices' partial sums, and copies of the operands
+// whose rows are no whole 16-byte units.
+struct WideLayout {
+    bool takes;
+    WidePlan plan;
+    int w_pitch, x_pitch;
+    bool pad_w, pad_x;
+    size_t partial, w_at, x_at, bytes;                 // bytes of the partial sums, offsets of the copies, all
+};
+
+WideLayout wide_layout(int64_t tokens, int64_t c_in, int64_t hidden, bool forward)
+{
+    WideLayout l{};
+    const int64_t k = forward ? c_in : 2 * hidden, c_pad = int64_t(round_up(c_in, 8)), k_pad = int64_t(round_up(k, 8));
+    l.w_pitch = int(c_pad);
+    l.x_pitch = int(k_pad);
+    l.pad_w = c_pad != c_in;
+    l.pad_x = k_pad != k;
+    l.plan = gated_wide_plan(tokens, c_pad, hidden, forward);
+    // Copies pay where the product is long (2 bytes an element in and out at 4 TB/s and a launch each, against the product of
+    // this file at 300 TFLOP/s forward and 50 backward, where it turns the weights element by element): 8192 tokens 4095 ->
+    // 10239 1140 us instead of 3500, the gradients of 4001 tokens 515 -> 1027 61 instead of 181
+    const double copies = (l.pad_w ? 4.0 + double(2 * hidden) * c_pad * 4 / 4e6 : 0.0) + (l.pad_x ? 4.0 + double(tokens) * k_pad * 4 / 4e6 : 0.0);
+    l.takes = l.plan.takes && (copies == 0.0 || l.plan.us + copies < 10.0 + 4.0 * double(tokens) * double(c_in) * double(hidden) / (forward ? 3e8 : 5e7));
+    if (!l.takes) return l;
+    l.partial = l.plan.splits == 1 ? 0 : round_up(size_t(l.plan.splits) * tokens * (forward ? 2 * hidden : c_in) * sizeof(float), 256);
+    l.w_at = l.partial;
+    l.x_at = l.w_at + (l.pad_w ? round_up(size_t(2 * hidden) * c_pad * 2, 256) : 0);
+    l.bytes = l.x_at + (l.pad_x ? round_up(size_t(tokens) * k_pad * 2, 256) : 0);
+    return l;
+}
+
+template <bool FORWARD>
+dropit_status launch_wide(GenArgs a, const WideLayout &l, void *workspace, hipStream_t stream)
+{
+    char *const ws = static_cast<char *>(workspace);
     WideArgs w{};
     w.w = a.w;
     w.x = a.x;
+    if (l.pad_w) {
+        launch_pad(a.w, 2 * int64_t(a.hidden), a.c_in, l.w_pitch, ws + l.w_at, stream);
+        w.w = ws + l.w_at;
+    }
+    if (l.pad_x) {
+        launch_pad(a.x, a.tokens, a.K, l.x_pitch, ws + l.x_at, stream);
+        w.x = ws + l.x_at;
+    }
+    w.w_pitch = l.w_pitch;
+    w.x_pitch = l.x_pitch;
     w.tokens = a.tokens;
     w.hidden = a.hidden;
     w.c_in = a.c_in;
-    w.K = a.K;
+    w.K = FORWARD ? l.x_pitch : a.K;
     w.act = a.act;
     w.bias = a.bias;
     w.out = a.out;
     w.pre = a.pre;
-    w.partial = a.partial;
-    w.splits = a.splits = plan.splits;
-    const dropit_status st = launch_gated_wide(w, plan, FORWARD, stream);
-    if (st != DROPIT_OK || plan.splits == 1) return st;
+    w.partial = a.partial = static_cast<float *>(workspace);
+    w.splits = a.splits = l.plan.splits;
+    const dropit_status st = launch_gated_wide(w, l.plan, FORWARD, stream);
+    if (st != DROPIT_OK || l.plan.splits == 1) return st;
     launch_finish<true, FORWARD>(a, stream);
     return launch_status();
 }
@@ -459,16 +520,22 @@ bool valid_sizes(int64_t tokens, int64_t c_in, int64_t hidden, dropit_dtype dt)
 size_t forward_bytes(int64_t tokens, int64_t c_in, int64_t hidden, dropit_dtype dt)
 {
     if (tokens == 0 || gated_tokens_takes(tokens, c_in, hidden, dt)) return 0;
-    const WidePlan plan = gated_wide_plan(tokens, c_in, hidden, true);
-    const int splits = dt == DROPIT_BF16 && plan.takes ? plan.splits : gen_splits(tokens, int(hidden), GEN_ROWS / 2, c_in);
+    if (dt == DROPIT_BF16) {
+        const WideLayout l = wide_layout(tokens, c_in, hidden, true);
+        if (l.takes) return l.bytes;
+    }
+    const int splits = gen_splits(tokens, int(hidden), GEN_ROWS / 2, c_in);
     return splits == 1 ? 0 : size_t(splits) * tokens * 2 * hidden * sizeof(float);
 }
 
 size_t dx_bytes(int64_t tokens, int64_t c_in, int64_t hidden, dropit_dtype dt)
 {
     if (tokens == 0) return 0;
-    const WidePlan plan = gated_wide_plan(tokens, c_in, hidden, false);
-    const int splits = dt == DROPIT_BF16 && plan.takes ? plan.splits : gen_splits(tokens, int(c_in), GEN_ROWS, 2 * hidden);
+    if (dt == DROPIT_BF16) {
+        const WideLayout l = wide_layout(tokens, c_in, hidden, false);
+        if (l.takes) return l.bytes;
+    }
+    const int splits = gen_splits(tokens, int(c_in), GEN_ROWS, 2 * hidden);
     return splits == 1 ? 0 : size_t(splits) * tokens * c_in * sizeof(float);
 }
 
@@ -508,8 +575,10 @@ extern "C" dropit_status dropit_gated_forward(const void *x, int64_t tokens, int
     a.pre = pre;
     a.partial = static_cast<float *>(workspace);
     if (gated_tokens_takes(tokens, c_in, hidden, dt)) return launch_gated_tokens(x, tokens, a.c_in, dt, w, bias, a.hidden, act, h, pre, stream);
-    const WidePlan plan = gated_wide_plan(tokens, c_in, hidden, true);
-    if (dt == DROPIT_BF16 && plan.takes) return launch_wide<true>(a, plan, stream);
+    if (dt == DROPIT_BF16) {
+        const WideLayout l = wide_layout(tokens, c_in, hidden, true);
+        if (l.takes) return launch_wide<true>(a, l, workspace, stream);
+    }
     return dt == DROPIT_BF16 ? launch_generic<true, true>(a, stream) : launch_generic<false, true>(a, stream);
 }
 
@@ -564,7 +633,9 @@ extern "C" dropit_status dropit_gated_backward(const void *dh, const void *pre, 
     a.act = act;
     a.out = dx;
     a.partial = static_cast<float *>(workspace);
-    const WidePlan plan = gated_wide_plan(tokens, c_in, hidden, false);
-    if (bf16 && plan.takes) return launch_wide<false>(a, plan, stream);
+    if (bf16) {
+        const WideLayout l = wide_layout(tokens, c_in, hidden, false);
+        if (l.takes) return launch_wide<false>(a, l, workspace, stream);
+    }
     return bf16 ? launch_generic<true, false>(a, stream) : launch_generic<false, false>(a, stream);
 }

@@ -125,7 +125,7 @@ gated_wide_kernel(const WideArgs a)
     constexpr uint32_t OUTSIDE = 0x80000000u;          // (gated_wide_takes: ranges are smaller)
     constexpr int per_tile = FORWARD ? WIDE_ROWS / 2 : WIDE_ROWS;   // output columns
     const int part = wave & 3;                         // of the group's tile
-    const uint32_t w_pitch = uint32_t(a.c_in) * 2u, x_pitch = uint32_t(a.K) * 2u;
+    const uint32_t w_pitch = uint32_t(a.w_pitch) * 2u, x_pitch = uint32_t(a.x_pitch) * 2u;
     // tile rows of 128 bytes: load q holds rows 8 (L part + q) + lane / 8 for L loads of a wavefront, whose units are turned by
     // (row / 2) % 8, that is by lane / 16 and, for odd q (L is even), by 4 more.  Forward weights: row R of a wavefront's 64
     // is gate row R for R < 32, then up rows of the same columns.  Tile rows of 512 bytes: load q holds k = 16 part + 2 q +
@@ -169,14 +169,14 @@ gated_wide_kernel(const WideArgs a)
         l_end = slice_begin(slice + 1);
         l_outside[0] = l_outside[1] = 0u;
         if (late) {
-            l_base = static_cast<const char *>(a.x) + int64_t(tt) * C::TOKENS * a.K * 2;
-            l_range = min(int(a.tokens) - tt * C::TOKENS, C::TOKENS) * a.K * 2;
+            l_base = static_cast<const char *>(a.x) + int64_t(tt) * C::TOKENS * a.x_pitch * 2;
+            l_range = min(int(a.tokens) - tt * C::TOKENS, C::TOKENS) * a.x_pitch * 2;
         } else if constexpr (FORWARD) {
-            l_base = static_cast<const char *>(a.w) + int64_t(rt) * per_tile * a.c_in * 2;
-            l_range = (2 * a.hidden - rt * per_tile) * a.c_in * 2;
+            l_base = static_cast<const char *>(a.w) + int64_t(rt) * per_tile * a.w_pitch * 2;
+            l_range = (2 * a.hidden - rt * per_tile) * a.w_pitch * 2;
         } else {
             l_base = static_cast<const char *>(a.w) + int64_t(rt) * per_tile * 2;
-            l_range = 2 * a.hidden * a.c_in * 2 - rt * per_tile * 2;
+            l_range = 2 * a.hidden * a.w_pitch * 2 - rt * per_tile * 2;
 #pragma unroll
             for (int o = 0; o < 2; ++o) l_outside[o] = uint32_t(rt * per_tile) * 2u + column[o] < w_pitch ? 0u : OUTSIDE;
         }
@@ -439,12 +439,10 @@ dropit_status launch(const WideArgs &a, hipStream_t stream)
 
 WidePlan gated_wide_plan(int64_t tokens, int64_t c_in, int64_t hidden, bool forward)
 {
-    // rows in 16-byte units; the weights, and 256 tokens, below 2^31 bytes.  Few tokens leave most of a tile empty, but its
+    // the weights, and 256 tokens, below 2^31 bytes.  Few tokens leave most of a tile empty, but its
     // slices fill the chip (us for the gradients of 16 tokens, here and in gated.hip's product: 384 -> 1024 15 and 19, 2048 ->
     // 5632 23 and 46, 4096 -> 10240 45 and 115)
-    WidePlan plan{(!forward || tokens > 32) && c_in % 8 == 0 && (forward || hidden % 4 == 0) && 4 * hidden * c_in < int64_t(1) << 31 &&
-                      std::max(c_in, 2 * hidden) < 1 << 22,
-                  2, 1};
+    WidePlan plan{(!forward || tokens > 32) && 4 * hidden * c_in < int64_t(1) << 31 && std::max(c_in, 2 * hidden) < (1 << 22) - 8, 2, 1, 0.0};
     if (!plan.takes) return plan;
     // How many tokens to a tile, and how many slices of the sum: what the compute unit with the most tiles takes, a block of
     // the sum and a tile's start and end at what they were measured to cost (us; whole chip busy: blocks of 8192 tokens 4096 ->
@@ -471,6 +469,7 @@ WidePlan gated_wide_plan(int64_t tokens, int64_t c_in, int64_t hidden, bool forw
             }
         }
     }
+    plan.us = best_us;
     return plan;
 }
 

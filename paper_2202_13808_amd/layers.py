@@ -7,6 +7,7 @@ formulas stand in the header.
 from __future__ import annotations
 
 import ctypes
+import functools
 import math
 from typing import NamedTuple, Optional, Sequence, Tuple, Union
 
@@ -45,15 +46,23 @@ def _like(t: Optional[torch.Tensor], shape, dtype: torch.dtype, device: torch.de
 
 
 def _check_tensors(first: torch.Tensor, *others: Optional[torch.Tensor]) -> None:
-    where = first.get_device()
-    for t in (first,) + others:
-        if t is not None:
-            if not t.is_cuda:
-                raise ValueError("dropit operates on device tensors only (no CPU path)")
-            if not t.is_contiguous():
-                raise ValueError("dropit tensors must be contiguous")
-            if t.get_device() != where:
-                raise ValueError("the tensors of a call must be on one device")
+    found = _marshal().describe([first] + [t for t in others if t is not None])
+    if found[4] == -2:
+        raise ValueError("the tensors of a call must be on one device")
+    if found[4] == -1:
+        raise ValueError("dropit operates on device tensors only (no CPU path)")
+    if not found[5]:
+        raise ValueError("dropit tensors must be contiguous")
+
+
+@functools.lru_cache(maxsize=4096)
+def _forward_bytes(tokens: int, c_in: int, hidden: int, code: int) -> int:
+    return int(lib().dropit_gated_forward_workspace_bytes(tokens, c_in, hidden, code))
+
+
+@functools.lru_cache(maxsize=4096)
+def _backward_bytes(tokens: int, c_in: int, hidden: int, code: int, need_dx: bool, need_dbias: bool) -> int:
+    return int(lib().dropit_gated_backward_workspace_bytes(tokens, c_in, hidden, code, int(need_dx), int(need_dbias)))
 
 
 def _area(workspace: Optional[torch.Tensor], need: int, device: torch.device) -> Tuple[Optional[int], int]:
@@ -80,7 +89,7 @@ def gated_forward(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Te
     h = _like(h, lead + (hidden,), x.dtype, x.device, "h")
     if save or pre is not None:
         pre = _like(pre, lead + (2 * hidden,), x.dtype, x.device, "pre")
-    need = int(lib().dropit_gated_forward_workspace_bytes(tokens, c_in, hidden, code))
+    need = _forward_bytes(tokens, c_in, hidden, code)
     area, size = _area(workspace, need, x.device)
     with _on(x.device):
         _check(lib().dropit_gated_forward(x.data_ptr(), tokens, c_in, code, weight.data_ptr(),
@@ -110,7 +119,7 @@ def gated_backward(dh: torch.Tensor, pre: torch.Tensor, weight: torch.Tensor, ac
         dx = _like(dx, lead + (c_in,), dh.dtype, dh.device, "dx")
     if need_dbias:
         dbias = _like(dbias, (2 * hidden,), torch.float32, dh.device, "dbias")
-    need = int(lib().dropit_gated_backward_workspace_bytes(tokens, c_in, hidden, code, int(need_dx), int(need_dbias)))
+    need = _backward_bytes(tokens, c_in, hidden, code, bool(need_dx), bool(need_dbias))
     area, size = _area(workspace, need, dh.device)
     with _on(dh.device):
         _check(lib().dropit_gated_backward(dh.data_ptr(), pre.data_ptr(), tokens, c_in, code, weight.data_ptr(), hidden, act_code,
@@ -266,23 +275,21 @@ def grad_norm(grads: Sequence[torch.Tensor], max_norm: float = math.inf, out: Op
     if count == 0:
         raise ValueError("grad_norm needs a tensor (it tells the device)")
     g = _read(grads, "gradients", (F32, BF16, -2))
-    device, dtypes = g.device, np.frombuffer(g.types, dtype=np.int32)
-    if g.type == -2 and not bool(((dtypes == F32) | (dtypes == BF16)).all()):
+    device = g.device
+    if g.type == -2 and not set(np.frombuffer(g.types, dtype=np.int32).tolist()) <= {F32, BF16}:
         raise TypeError("dropit supports float32 and bfloat16 tensors, got %s" % sorted({str(t.dtype) for t in grads}))
     where = grads[0].device
     if out is None:
         out = torch.empty(2, dtype=torch.float32, device=where)
     elif out.dtype != torch.float32 or out.numel() < 2 or out.get_device() != device or not out.is_contiguous():
         raise ValueError("out must hold two contiguous float32 elements on the gradients' device")
-    pointers, numels = _int64(g.pointers), _int64(g.numels)
-    at_pointers, at_numels = pointers.ctypes.data, numels.ctypes.data
-    need = int(lib().dropit_grad_norm_workspace_bytes(at_numels, count))
+    need = int(lib().dropit_grad_norm_workspace_bytes(g.numels, count))      # (bytes arrive as pointers to them)
     if workspace is None:
         workspace = torch.empty(need, dtype=torch.uint8, device=where) if need else None
     else:
         _require_device(workspace)
     with _on(where):
-        _check(lib().dropit_grad_norm(at_pointers, at_numels, dtypes.ctypes.data, count, float(max_norm),
+        _check(lib().dropit_grad_norm(g.pointers, g.numels, g.types, count, float(max_norm),
                                       out.data_ptr(), workspace.data_ptr() if workspace is not None else None,
                                       workspace.numel() if workspace is not None else 0, _stream_ptr(stream, where)))
     return out

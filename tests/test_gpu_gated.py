@@ -131,6 +131,14 @@ def test_sizes(tokens, c, hidden, dtype):
     run_case(tokens, c, hidden, dtype, "silu", bias=hidden % 2 == 0)
 
 
+@pytest.mark.parametrize("tokens,c,hidden", [
+    (4001, 515, 1027), (2500, 1030, 770),              # rows that are no whole 16-byte units, copied into such
+    (100, 2048, 131), (70, 4096, 40),                  # few tiles: the sum in slices, odd width and even
+    (16384, 64, 512), (32768, 512, 32), (12608, 128, 2048)])           # 256 and 192 tokens to a tile, several tiles a workgroup
+def test_larger_products(tokens, c, hidden):
+    run_case(tokens, c, hidden, "bf16", "gelu", bias=True, seed=6)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("act", ACTS)
 def test_activations(act, dtype):
