@@ -16,11 +16,14 @@ namespace dropit {
 namespace {
 
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 // sixteen bytes at any element's address: a row of odd length moves in wide accesses too
 typedef u32x4 u32x4_any __attribute__((aligned(2)));
+typedef u32x2 u32x2_any __attribute__((aligned(2)));
 
 template <bool BF16> struct Elem { using type = float; static constexpr int PER16 = 4; };
 template <> struct Elem<true> { using type = uint16_t; static constexpr int PER16 = 8; };
@@ -36,11 +39,28 @@ template <bool BF16> __device__ inline void store_one(void *p, int64_t i, float 
     else static_cast<float *>(p)[i] = v;
 }
 
+// the first `some` (four, where there are more) of four consecutive elements
+template <bool BF16> __device__ inline void store_four(void *p, int64_t i, const f32x4 &v, int some)
+{
+    if (some < 4) {
+        for (int e = 0; e < some; ++e) store_one<BF16>(p, i + e, v[e]);
+        return;
+    }
+    if constexpr (BF16) {
+        bf16x4 b;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) b[e] = static_cast<__bf16>(v[e]);
+        *reinterpret_cast<u32x2_any *>(static_cast<uint16_t *>(p) + i) = __builtin_bit_cast(u32x2, b);
+    } else {
+        *reinterpret_cast<u32x4_any *>(static_cast<float *>(p) + i) = __builtin_bit_cast(u32x4, v);
+    }
+}
+
 // ---------------------------------------------------------------------------
-// The product for every size and type: tiles of 64 tokens by 128 rows of the weight operand, four wavefronts of 64 x 32.
-// fp32 runs on the fp32 matrix instructions.
+// The product for every size and type: tiles of 64 tokens by 64 rows of the weight operand, four wavefronts of 32 x 32, in the
+// forward pass 16 gate and 16 up rows each.  fp32 runs on the fp32 matrix instructions.
 // Few tiles: the sum is cut into slices, whose partial sums finish_kernel adds in ascending order.
-constexpr int GEN_THREADS = 256, GEN_ROWS = 128, GEN_TOKENS = 64, GEN_K = 32;
+constexpr int GEN_THREADS = 256, GEN_ROWS = 64, GEN_TOKENS = 64, GEN_K = 32;
 
 struct GenArgs {
     const void *w, *x;          // weight operand; token operand [tokens][K]
@@ -54,20 +74,17 @@ struct GenArgs {
     int splits, row_tiles;
 };
 
-// sixteen bytes of row `row` of a K-contiguous operand from element k on, zeros past the end
+// sixteen bytes of a row from element k on, zeros from `end` on (which may be 0): element by element and without a branch
 template <bool BF16>
-__device__ inline u32x4 load_unit(const void *base, int64_t row, int64_t pitch, int k, int end)
+__device__ inline u32x4 load_elements(const typename Elem<BF16>::type *row, int k, int end)
 {
-    constexpr int PER = Elem<BF16>::PER16;
-    const auto *p = static_cast<const typename Elem<BF16>::type *>(base) + row * pitch + k;
-    if (k + PER <= end) return *reinterpret_cast<const u32x4_any *>(p);
     u32x4 r = {0u, 0u, 0u, 0u};
 #pragma unroll
-    for (int e = 0; e < PER; ++e)
-        if (k + e < end) {
-            if constexpr (BF16) r[e >> 1] |= uint32_t(p[e]) << (16 * (e & 1));
-            else r[e] = __float_as_uint(p[e]);
-        }
+    for (int e = 0; e < Elem<BF16>::PER16; ++e) {
+        const auto v = row[max(min(k + e, end - 1), 0)];
+        if constexpr (BF16) r[e >> 1] |= (k + e < end ? uint32_t(v) : 0u) << (16 * (e & 1));
+        else r[e] = k + e < end ? __float_as_uint(v) : 0u;
+    }
     return r;
 }
 
@@ -94,74 +111,103 @@ gated_product_kernel(const GenArgs a)
     const int steps_all = (a.K + GEN_K - 1) / GEN_K;
     const int s0 = int(int64_t(steps_all) * split / a.splits), s1 = int(int64_t(steps_all) * (split + 1) / a.splits);
 
-    // weight row of the tile's row R: forward, wavefront row R / 64 takes 32 gate rows and the 32 up rows of the same columns
+    // weight row of the tile's row R: forward, a wavefront's rows are HALF gate rows and the HALF up rows of the same columns
+    constexpr int HALF = GEN_ROWS / 4;
     auto weight_row = [&](int R) -> int64_t {
-        const int n = min(r0 + (R >> 6) * 32 + (R & 31), a.hidden - 1);
-        return (R & 32) ? int64_t(a.hidden) + n : n;
+        const int n = min(r0 + R / (2 * HALF) * HALF + R % HALF, a.hidden - 1);
+        return (R & HALF) ? int64_t(a.hidden) + n : n;
     };
-    u32x4 ra[A_LOADS], rb[B_LOADS];
-    auto load = [&](int s) {
+    // where a thread's units start; from one step to the next they move by 32 elements, or by 32 rows of W
+    using T = typename Elem<BF16>::type;
+    const T *wp[A_LOADS], *xp[B_LOADS];
+    const int64_t w_step = FORWARD ? GEN_K : int64_t(GEN_K) * a.c_in;
+#pragma unroll
+    for (int i = 0; i < A_LOADS; ++i) {
+        const int unit = i * GEN_THREADS + tid;
+        if constexpr (FORWARD) {
+            wp[i] = static_cast<const T *>(a.w) + weight_row(unit / UNITS) * a.c_in + unit % UNITS * PER;
+        } else {
+            const int c = r0 + unit % (GEN_ROWS / PER) * PER;
+            wp[i] = static_cast<const T *>(a.w) + int64_t(unit / (GEN_ROWS / PER)) * a.c_in + (c < a.c_in ? c : 0);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < B_LOADS; ++i) {
+        const int unit = i * GEN_THREADS + tid;
+        xp[i] = static_cast<const T *>(a.x) + min<int64_t>(t0 + unit / UNITS, a.tokens - 1) * a.K + unit % UNITS * PER;
+    }
+    // Steps whose units pass no end: the input gradient's units that pass the end of a row of W take what follows there, for columns
+    // that are not stored, so that step has to end a unit before the end of W.
+    const int whole = FORWARD || a.c_in % PER == 0 ? a.K / GEN_K : (a.K - (PER + a.c_in - 1) / a.c_in) / GEN_K;
+    struct Units {
+        u32x4 a[A_LOADS], b[B_LOADS];
+    };
+    auto load = [&](int s, Units &r) {
+#pragma unroll
+        for (int i = 0; i < A_LOADS; ++i) r.a[i] = *reinterpret_cast<const u32x4_any *>(wp[i] + s * w_step);
+#pragma unroll
+        for (int i = 0; i < B_LOADS; ++i) r.b[i] = *reinterpret_cast<const u32x4_any *>(xp[i] + s * GEN_K);
+    };
+    // any step, element by element: nothing past the end of a row is read, and zeros stand there
+    auto load_last = [&](int s, Units &r) {
         const int k0 = s * GEN_K;
 #pragma unroll
         for (int i = 0; i < A_LOADS; ++i) {
-            const int unit = i * GEN_THREADS + tid;
-            if constexpr (FORWARD) {
-                ra[i] = load_unit<BF16>(a.w, weight_row(unit / UNITS), a.c_in, k0 + unit % UNITS * PER, a.K);
-            } else {                                                // W [K][c_in]: a unit is PER columns of one k
-                const int k = k0 + unit / (GEN_ROWS / PER), c = r0 + unit % (GEN_ROWS / PER) * PER;
-                ra[i] = k < a.K && c < a.c_in ? load_unit<BF16>(a.w, k, a.c_in, c, a.c_in) : u32x4{0u, 0u, 0u, 0u};
+            const int unit = i * GEN_THREADS + tid, k = k0 + (FORWARD ? unit % UNITS * PER : unit / (GEN_ROWS / PER));
+            if constexpr (FORWARD) r.a[i] = load_elements<BF16>(wp[i] - unit % UNITS * PER, k, a.K);
+            else {                                                  // W [K][c_in]: a unit is PER columns of one k
+                const int c = r0 + unit % (GEN_ROWS / PER) * PER;
+                r.a[i] = load_elements<BF16>(static_cast<const T *>(a.w) + int64_t(min(k, a.K - 1)) * a.c_in, c, k < a.K ? a.c_in : 0);
             }
         }
 #pragma unroll
         for (int i = 0; i < B_LOADS; ++i) {
-            const int unit = i * GEN_THREADS + tid;
-            rb[i] = load_unit<BF16>(a.x, min<int64_t>(t0 + unit / UNITS, a.tokens - 1), a.K, k0 + unit % UNITS * PER, a.K);
+            const int at = (i * GEN_THREADS + tid) % UNITS * PER;
+            r.b[i] = load_elements<BF16>(xp[i] - at, k0 + at, a.K);
         }
     };
-    auto put = [&](char *to) {
+    auto put = [&](char *to, const Units &r) {
 #pragma unroll
         for (int i = 0; i < A_LOADS; ++i) {
             const int unit = i * GEN_THREADS + tid;
             if constexpr (FORWARD) {
-                *reinterpret_cast<u32x4 *>(to + unit / UNITS * PITCH + unit % UNITS * 16) = ra[i];
+                *reinterpret_cast<u32x4 *>(to + unit / UNITS * PITCH + unit % UNITS * 16) = r.a[i];
             } else {
                 const int k = unit / (GEN_ROWS / PER), c = unit % (GEN_ROWS / PER) * PER;
-                if constexpr (AS_IT_LIES) *reinterpret_cast<u32x4 *>(to + k * K_PITCH + c * ES) = ra[i];
+                if constexpr (AS_IT_LIES) *reinterpret_cast<u32x4 *>(to + k * K_PITCH + c * ES) = r.a[i];
                 else
 #pragma unroll
                 for (int e = 0; e < PER; ++e) {
                     char *at = to + (c + e) * PITCH + k * ES;
-                    *reinterpret_cast<uint16_t *>(at) = uint16_t(ra[i][e >> 1] >> (16 * (e & 1)));
+                    *reinterpret_cast<uint16_t *>(at) = uint16_t(r.a[i][e >> 1] >> (16 * (e & 1)));
                 }
             }
         }
 #pragma unroll
         for (int i = 0; i < B_LOADS; ++i) {
             const int unit = i * GEN_THREADS + tid;
-            *reinterpret_cast<u32x4 *>(to + A_BYTES + unit / UNITS * PITCH + unit % UNITS * 16) = rb[i];
+            *reinterpret_cast<u32x4 *>(to + A_BYTES + unit / UNITS * PITCH + unit % UNITS * 16) = r.b[i];
         }
     };
 
-    f32x16 acc[2];
+    f32x16 acc;
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) acc[i][e] = 0.f;
-    if (s0 < s1) load(s0);
-    for (int s = s0; s < s1; ++s) {
-        char *cur = tile[(s - s0) & 1];
-        put(cur);
+    for (int e = 0; e < 16; ++e) acc[e] = 0.f;
+    int turn = 0;
+    auto put_and_wait = [&](const Units &r) {
+        put(tile[turn], r);
         __syncthreads();                                            // (the other tile's readers passed the barrier before)
-        if (s + 1 < s1) load(s + 1);
-        const char *wa = cur + (wm * 64 + (lane & 31)) * PITCH, *xb = cur + A_BYTES + (wn * 32 + (lane & 31)) * PITCH;
+    };
+    auto multiply = [&]() {
+        const char *cur = tile[turn];
+        turn ^= 1;
+        const char *wa = cur + (wm * 32 + (lane & 31)) * PITCH, *xb = cur + A_BYTES + (wn * 32 + (lane & 31)) * PITCH;
         if constexpr (BF16) {
 #pragma unroll
             for (int kk = 0; kk < GEN_K / 16; ++kk) {
                 const int at = kk * 32 + (lane >> 5) * 16;
                 const bf16x8 b = *reinterpret_cast<const bf16x8 *>(xb + at);
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-                    acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(wa + i * 32 * PITCH + at), b, acc[i], 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(wa + at), b, acc, 0, 0, 0);
             }
         } else {
             // an instruction takes one k from each half of the wavefront: k = 8 kk + e and 8 kk + 4 + e
@@ -169,61 +215,90 @@ gated_product_kernel(const GenArgs a)
             for (int kk = 0; kk < GEN_K / 8; ++kk) {
                 const int at = kk * 32 + (lane >> 5) * 16;
                 const f32x4 b = *reinterpret_cast<const f32x4 *>(xb + at);
-                f32x4 w[2];
+                f32x4 w;
+                if constexpr (AS_IT_LIES) {
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    if constexpr (AS_IT_LIES) {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            w[i][e] = *reinterpret_cast<const float *>(cur + (kk * 8 + (lane >> 5) * 4 + e) * K_PITCH + (wm * 64 + i * 32 + (lane & 31)) * ES);
-                    } else {
-                        w[i] = *reinterpret_cast<const f32x4 *>(wa + i * 32 * PITCH + at);
-                    }
+                    for (int e = 0; e < 4; ++e)
+                        w[e] = *reinterpret_cast<const float *>(cur + (kk * 8 + (lane >> 5) * 4 + e) * K_PITCH + (wm * 32 + (lane & 31)) * ES);
+                } else {
+                    w = *reinterpret_cast<const f32x4 *>(wa + at);
                 }
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) acc[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(w[i][e], b[e], acc[i], 0, 0, 0);
+                for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(w[e], b[e], acc, 0, 0, 0);
             }
         }
+    };
+    // Two steps are on their way while one is multiplied; loads behind the last whole step repeat it, so that no branch stands
+    // between a load and its wait.  What is no whole step comes first, under the others' first loads.
+    Units even, odd;
+    const int end = min(s1, whole);
+    if (s0 < end) {
+        load(s0, even);
+        load(min(s0 + 1, end - 1), odd);
     }
-    // lane l holds token l % 32 and, in register 4 q + e, row 8 q + 4 (l / 32) + e of each 32 x 32 block
+    for (int s = max(s0, whole); s < s1; ++s) {
+        Units last;
+        load_last(s, last);
+        put_and_wait(last);
+        multiply();
+    }
+    for (int s = s0; s < end;) {
+        put_and_wait(even);
+        load(min(s + 2, end - 1), even);
+        multiply();
+        if (++s >= end) break;
+        put_and_wait(odd);
+        load(min(s + 2, end - 1), odd);
+        multiply();
+        ++s;
+    }
+    // lane l holds token l % 32 and, in register 4 q + e, row 8 q + 4 (l / 32) + e of each 32 x 32 block: four consecutive output
+    // columns, stored in one access (one store an element made the stores, 64 rows each, longer than the product)
     const int64_t t = t0 + wn * 32 + (lane & 31);
     if (t >= a.tokens) return;
+    if constexpr (FORWARD) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
+        for (int q = 0; q < 2; ++q) {                               // the up row of gate row m is row m + 16, register 4 (q + 2) + e
+            const int n = r0 + wm * HALF + q * 8 + (lane >> 5) * 4, some = a.hidden - n;
+            if (some <= 0) continue;
+            f32x4 g, u, h;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int m = q * 8 + (lane >> 5) * 4 + e;
-            if constexpr (FORWARD) {
-                const int n = r0 + wm * 32 + m;
-                if (n >= a.hidden) continue;
-                float g = acc[0][q * 4 + e], u = acc[1][q * 4 + e];
-                if (a.partial != nullptr) {
-                    float *to = a.partial + (int64_t(split) * a.tokens + t) * 2 * a.hidden;
-                    to[n] = g;
-                    to[a.hidden + n] = u;
-                    continue;
-                }
-                if (a.bias != nullptr) {
-                    g += load_one<BF16>(a.bias, n);
-                    u += load_one<BF16>(a.bias, int64_t(a.hidden) + n);
-                }
-                store_one<BF16>(a.out, t * a.hidden + n, activation<BF16>(g, a.act) * u);
-                if (a.pre != nullptr) {
-                    store_one<BF16>(a.pre, t * 2 * a.hidden + n, g);
-                    store_one<BF16>(a.pre, t * 2 * a.hidden + a.hidden + n, u);
-                }
-            } else {
+            for (int e = 0; e < 4; ++e) {
+                g[e] = acc[q * 4 + e];
+                u[e] = acc[q * 4 + 8 + e];
+            }
+            if (a.partial != nullptr) {
+                float *to = a.partial + (int64_t(split) * a.tokens + t) * 2 * a.hidden + n;
+                store_four<false>(to, 0, g, some);
+                store_four<false>(to, a.hidden, u, some);
+                continue;
+            }
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const int c = r0 + wm * 64 + i * 32 + m;
-                    if (c >= a.c_in) continue;
-                    if (a.partial != nullptr) a.partial[(int64_t(split) * a.tokens + t) * a.c_in + c] = acc[i][q * 4 + e];
-                    else store_one<BF16>(a.out, t * a.c_in + c, acc[i][q * 4 + e]);
+            for (int e = 0; e < 4; ++e) {
+                if (a.bias != nullptr && e < some) {
+                    g[e] += load_one<BF16>(a.bias, n + e);
+                    u[e] += load_one<BF16>(a.bias, int64_t(a.hidden) + n + e);
                 }
+                h[e] = activation<BF16>(g[e], a.act) * u[e];
+            }
+            store_four<BF16>(a.out, t * a.hidden + n, h, some);
+            if (a.pre != nullptr) {
+                store_four<BF16>(a.pre, t * 2 * a.hidden + n, g, some);
+                store_four<BF16>(a.pre, t * 2 * a.hidden + a.hidden + n, u, some);
             }
         }
+    } else {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int c = r0 + wm * 32 + q * 8 + (lane >> 5) * 4, some = a.c_in - c;
+            if (some <= 0) continue;
+            f32x4 v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = acc[q * 4 + e];
+            if (a.partial != nullptr) store_four<false>(a.partial, (int64_t(split) * a.tokens + t) * a.c_in + c, v, some);
+            else store_four<BF16>(a.out, t * a.c_in + c, v, some);
+        }
+    }
 }
 
 // Adds the slices' partial sums in ascending order and finishes: bias, activation and product, or the rounding of dx.
@@ -261,13 +336,22 @@ gated_finish_kernel(const GenArgs a)
     }
 }
 
-// Slices of the sum: enough workgroups for two on each of 256 compute units, at least eight steps of 32 in a slice (below
-// that a slice is mostly its own start and end).
-int gen_splits(int64_t tokens, int rows, int per_tile, int64_t K)
+// Slices of the sum, at least eight steps of 32 in each (below that a slice is mostly its own start and end): enough workgroups for
+// three on each of 256 compute units, as two leave a third of the time in waits where there is room for more (fp32, us, two and
+// three: the gradient of 4000 tokens 384 -> 1024 84 and 74, of 1576 tokens 38.4 and 37.4, four 74 and 39.7).  fp32 products whose
+// tiles leave compute units empty take slices of four steps (70 tokens 384 -> 1024 12.2 and 9.4 us; bf16 7.2 and 8.5 at 200 tokens
+// 387 -> 515: its steps are shorter than what the second kernel costs).
+struct GenPlan {
+    int row_tiles, splits;
+};
+GenPlan gen_plan(int64_t tokens, int64_t c_in, int64_t hidden, dropit_dtype dt, bool forward)
 {
-    const int64_t tiles = (tokens + GEN_TOKENS - 1) / GEN_TOKENS * ((rows + per_tile - 1) / per_tile);
-    const int64_t steps = (K + GEN_K - 1) / GEN_K;
-    return int(std::max<int64_t>(1, std::min<int64_t>(512 / tiles, steps / 8)));
+    const int64_t across = forward ? 2 * hidden : c_in, K = forward ? c_in : 2 * hidden;
+    const int64_t row_tiles = (across + GEN_ROWS - 1) / GEN_ROWS, steps = (K + GEN_K - 1) / GEN_K;
+    const int64_t tiles = (tokens + GEN_TOKENS - 1) / GEN_TOKENS * row_tiles;
+    int64_t splits = std::max<int64_t>(1, std::min(768 / tiles, steps / 8));
+    if (dt == DROPIT_F32) splits = std::max(splits, std::min(256 / tiles, steps / 4));
+    return GenPlan{int(row_tiles), int(splits)};
 }
 
 template <bool BF16, bool FORWARD>
@@ -280,13 +364,11 @@ void launch_finish(const GenArgs &a, hipStream_t stream)
 template <bool BF16, bool FORWARD>
 dropit_status launch_generic(GenArgs a, hipStream_t stream)
 {
-    constexpr int per_tile = FORWARD ? GEN_ROWS / 2 : GEN_ROWS;
-    const int rows = FORWARD ? a.hidden : a.c_in;
-    a.row_tiles = (rows + per_tile - 1) / per_tile;
-    a.splits = gen_splits(a.tokens, rows, per_tile, a.K);
+    const GenPlan plan = gen_plan(a.tokens, a.c_in, a.hidden, BF16 ? DROPIT_BF16 : DROPIT_F32, FORWARD);
+    a.row_tiles = plan.row_tiles;
+    a.splits = plan.splits;
     if (a.splits == 1) a.partial = nullptr;
-    const int64_t tiles = (a.tokens + GEN_TOKENS - 1) / GEN_TOKENS * a.row_tiles;
-    const dim3 grid(static_cast<uint32_t>(tiles), a.splits);
+    const dim3 grid(static_cast<uint32_t>((a.tokens + GEN_TOKENS - 1) / GEN_TOKENS * plan.row_tiles), a.splits);
     gated_product_kernel<BF16, FORWARD><<<grid, GEN_THREADS, 0, stream>>>(a);
     if (a.splits > 1) launch_finish<BF16, FORWARD>(a, stream);
     return launch_status();
@@ -294,21 +376,22 @@ dropit_status launch_generic(GenArgs a, hipStream_t stream)
 
 // Rows of any length into rows of whole 16-byte units, zeros behind the end.
 __global__ void __launch_bounds__(256)
-gated_pad_kernel(const void *__restrict__ from, int64_t rows, int length, int pitch, uint16_t *__restrict__ to)
+gated_pad_kernel(const uint16_t *__restrict__ from, int64_t rows, int length, int pitch, uint16_t *__restrict__ to)
 {
     const int units = pitch / 8;
     const int64_t total = rows * units;
     for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < total; i += int64_t(gridDim.x) * 256) {
         const int64_t r = i / units;
         const int k = int(i - r * units) * 8;
-        *reinterpret_cast<u32x4 *>(to + r * pitch + k) = load_unit<true>(from, r, length, k, length);
+        *reinterpret_cast<u32x4 *>(to + r * pitch + k) =
+            k + 8 <= length ? *reinterpret_cast<const u32x4_any *>(from + r * length + k) : load_elements<true>(from + r * length, k, length);
     }
 }
 
 void launch_pad(const void *from, int64_t rows, int length, int pitch, void *to, hipStream_t stream)
 {
     const int64_t blocks = (rows * (pitch / 8) + 255) / 256;
-    gated_pad_kernel<<<static_cast<uint32_t>(std::min<int64_t>(blocks, 1 << 16)), 256, 0, stream>>>(from, rows, length, pitch, static_cast<uint16_t *>(to));
+    gated_pad_kernel<<<static_cast<uint32_t>(std::min<int64_t>(blocks, 1 << 16)), 256, 0, stream>>>(static_cast<const uint16_t *>(from), rows, length, pitch, static_cast<uint16_t *>(to));
 }
 
 // Whether a product runs on wide tiles, and what it keeps in the workspace: the slices' partial sums, and copies of the operands
@@ -485,6 +568,7 @@ gated_bias_kernel(const float *__restrict__ partial, int64_t blocks, int64_t wid
     const int64_t n = int64_t(blockIdx.x) * 16 + col;
     float s = 0.f;
     if (n < width)
+#pragma unroll 8
         for (int64_t b = part; b < blocks; b += 16) s += partial[b * width + n];
     red[part][col] = s;
     __syncthreads();
@@ -513,7 +597,7 @@ bool valid_sizes(int64_t tokens, int64_t c_in, int64_t hidden, dropit_dtype dt)
     if (tokens < 0 || tokens > INT32_MAX || c_in < 1 || c_in > 1 << 28 || hidden < 1 || hidden > 1 << 27) return false;
     if (dt != DROPIT_F32 && dt != DROPIT_BF16) return false;
     // a launch has fewer than 2^32 threads
-    const int64_t across = std::max((hidden + GEN_ROWS / 2 - 1) / (GEN_ROWS / 2), (c_in + GEN_ROWS - 1) / GEN_ROWS);
+    const int64_t across = std::max((2 * hidden + GEN_ROWS - 1) / GEN_ROWS, (c_in + GEN_ROWS - 1) / GEN_ROWS);
     return (tokens + GEN_TOKENS - 1) / GEN_TOKENS * across <= 1 << 23;
 }
 
@@ -524,7 +608,7 @@ size_t forward_bytes(int64_t tokens, int64_t c_in, int64_t hidden, dropit_dtype 
         const WideLayout l = wide_layout(tokens, c_in, hidden, true);
         if (l.takes) return l.bytes;
     }
-    const int splits = gen_splits(tokens, int(hidden), GEN_ROWS / 2, c_in);
+    const int splits = gen_plan(tokens, c_in, hidden, dt, true).splits;
     return splits == 1 ? 0 : size_t(splits) * tokens * 2 * hidden * sizeof(float);
 }
 
@@ -535,7 +619,7 @@ size_t dx_bytes(int64_t tokens, int64_t c_in, int64_t hidden, dropit_dtype dt)
         const WideLayout l = wide_layout(tokens, c_in, hidden, false);
         if (l.takes) return l.bytes;
     }
-    const int splits = gen_splits(tokens, int(c_in), GEN_ROWS, 2 * hidden);
+    const int splits = gen_plan(tokens, c_in, hidden, dt, false).splits;
     return splits == 1 ? 0 : size_t(splits) * tokens * c_in * sizeof(float);
 }
 
