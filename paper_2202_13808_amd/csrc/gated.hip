@@ -413,11 +413,12 @@ WideLayout wide_layout(int64_t tokens, int64_t c_in, int64_t hidden, bool forwar
     l.pad_w = c_pad != c_in;
     l.pad_x = k_pad != k;
     l.plan = gated_wide_plan(tokens, c_pad, hidden, forward);
-    // Copies pay where the product is long (2 bytes an element in and out at 4 TB/s and a launch each, against the product of
-    // this file at 300 TFLOP/s forward and 50 backward, where it turns the weights element by element): 8192 tokens 4095 ->
-    // 10239 1140 us instead of 3500, the gradients of 4001 tokens 515 -> 1027 61 instead of 181
+    // Copies pay where the product is long: 2 bytes an element in and out at 4 TB/s and a launch each, against the product of this
+    // file, which took 6 us and 230 TFLOP/s forward, 12 us and 180 backward, where it turns the weights element by element.  Both,
+    // us: 8192 tokens 1111 -> 2777 122 and 431 forward, 126 and 452 backward; 300 tokens 34 and 22, 42 and 31.
     const double copies = (l.pad_w ? 4.0 + double(2 * hidden) * c_pad * 4 / 4e6 : 0.0) + (l.pad_x ? 4.0 + double(tokens) * k_pad * 4 / 4e6 : 0.0);
-    l.takes = l.plan.takes && (copies == 0.0 || l.plan.us + copies < 10.0 + 4.0 * double(tokens) * double(c_in) * double(hidden) / (forward ? 3e8 : 5e7));
+    const double work = 4.0 * double(tokens) * double(c_in) * double(hidden), here = forward ? 6.0 + work / 2.3e8 : 12.0 + work / 1.8e8;
+    l.takes = l.plan.takes && (copies == 0.0 || l.plan.us + copies < here);
     if (!l.takes) return l;
     l.partial = l.plan.splits == 1 ? 0 : round_up(size_t(l.plan.splits) * tokens * (forward ? 2 * hidden : c_in) * sizeof(float), 256);
     l.w_at = l.partial;
