@@ -599,7 +599,7 @@ bool valid_sizes(int64_t tokens, int64_t c_in, int64_t hidden, dropit_dtype dt)
     if (dt != DROPIT_F32 && dt != DROPIT_BF16) return false;
     // a launch has fewer than 2^32 threads
     const int64_t across = std::max((2 * hidden + GEN_ROWS - 1) / GEN_ROWS, (c_in + GEN_ROWS - 1) / GEN_ROWS);
-    return (tokens + GEN_TOKENS - 1) / GEN_TOKENS * across <= 1 << 23;
+    return (tokens + GEN_TOKENS - 1) / GEN_TOKENS * across < 1 << 24;
 }
 
 size_t forward_bytes(int64_t tokens, int64_t c_in, int64_t hidden, dropit_dtype dt)

@@ -1,8 +1,9 @@
 """ctypes binding of the C ABI in ``include/dropit_layers.h`` -- marshalling and checks only.
 
 The operators that stand beside the dropped cache in a training step: the gated projection of a feed-forward block
-and its backward pass, the AdamW step over many tensors, the global gradient norm.  Functions have the names of the C entry points without the ``dropit_`` prefix; the
-formulas stand in the header.
+and its backward pass, the AdamW step over many tensors, the global gradient norm.  Functions have the names of the C
+entry points without the ``dropit_`` prefix; the formulas stand in the header.  ``stream`` (None: the current one) is a
+stream of the tensors' device that the inputs are ready on; outputs and workspaces are allocated for it.
 """
 from __future__ import annotations
 
@@ -65,6 +66,11 @@ def _backward_bytes(tokens: int, c_in: int, hidden: int, code: int, need_dx: boo
     return int(lib().dropit_gated_backward_workspace_bytes(tokens, c_in, hidden, code, int(need_dx), int(need_dbias)))
 
 
+def _check_stream(stream, device: torch.device) -> None:
+    if stream.device != device:
+        raise ValueError("the stream is on %s, the tensors are on %s" % (stream.device, device))
+
+
 def _area(workspace: Optional[torch.Tensor], need: int, device: torch.device) -> Tuple[Optional[int], int]:
     if workspace is None:
         if need == 0:
@@ -85,6 +91,10 @@ def gated_forward(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Te
         raise ValueError("weight and bias must have x's dtype, bias 2 * hidden = %d elements" % (2 * hidden))
     if x.dim() < 1 or x.shape[-1] != c_in:
         raise ValueError("x must be [..., %d], got %s" % (c_in, tuple(x.shape)))
+    if stream is not None:                             # what the call allocates has to belong to its stream too
+        _check_stream(stream, x.device)
+        with torch.cuda.stream(stream):
+            return gated_forward(x, weight, bias, act, save, h, pre, workspace)
     lead, tokens = tuple(x.shape[:-1]), x.numel() // c_in
     h = _like(h, lead + (hidden,), x.dtype, x.device, "h")
     if save or pre is not None:
@@ -95,7 +105,7 @@ def gated_forward(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Te
         _check(lib().dropit_gated_forward(x.data_ptr(), tokens, c_in, code, weight.data_ptr(),
                                           bias.data_ptr() if bias is not None else None, hidden, act_code, h.data_ptr(),
                                           pre.data_ptr() if pre is not None else None, area, size,
-                                          _stream_ptr(stream, x.device)))
+                                          _stream_ptr(None, x.device)))
     return (h, pre) if pre is not None else h
 
 
@@ -112,6 +122,10 @@ def gated_backward(dh: torch.Tensor, pre: torch.Tensor, weight: torch.Tensor, ac
         raise ValueError("pre and weight must have dh's dtype")
     if dh.dim() < 1 or dh.shape[-1] != hidden or tuple(pre.shape) != tuple(dh.shape[:-1]) + (2 * hidden,):
         raise ValueError("dh must be [..., %d] and pre [..., %d], got %s and %s" % (hidden, 2 * hidden, tuple(dh.shape), tuple(pre.shape)))
+    if stream is not None:
+        _check_stream(stream, dh.device)
+        with torch.cuda.stream(stream):
+            return gated_backward(dh, pre, weight, act, need_dx, need_dbias, dpre, dx, dbias, workspace)
     lead, tokens = tuple(dh.shape[:-1]), dh.numel() // hidden
     dpre = _like(dpre, lead + (2 * hidden,), dh.dtype, dh.device, "dpre")
     need_dx, need_dbias = need_dx or dx is not None, need_dbias or dbias is not None
@@ -125,7 +139,7 @@ def gated_backward(dh: torch.Tensor, pre: torch.Tensor, weight: torch.Tensor, ac
         _check(lib().dropit_gated_backward(dh.data_ptr(), pre.data_ptr(), tokens, c_in, code, weight.data_ptr(), hidden, act_code,
                                            dpre.data_ptr(), dx.data_ptr() if need_dx else None,
                                            dbias.data_ptr() if need_dbias else None, area, size,
-                                           _stream_ptr(stream, dh.device)))
+                                           _stream_ptr(None, dh.device)))
     return dpre, dx if need_dx else None, dbias if need_dbias else None
 
 
@@ -240,6 +254,8 @@ def adamw(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], m: Sequ
                         _scalar(step, torch.int32, device, "step") if isinstance(step, torch.Tensor) else None,
                         _scalar(grad_scale, torch.float32, device, "grad_scale"))
     where = params[0].device
+    if stream is not None:
+        _check_stream(stream, where)
     with _on(where):
         _check(lib().dropit_adamw(table.ctypes.data, count, p.type, columns[0][2].type, 8 if bits8 else 32,
                                   ctypes.byref(hyper), _stream_ptr(stream, where)))
@@ -255,13 +271,17 @@ def adamw_unpack(codes: torch.Tensor, offset: torch.Tensor, signed: bool, values
         raise ValueError("codes must be uint8 with an int16 offset for every %d of them" % ADAMW_BLOCK)
     if offset.device != codes.device or (values is not None and values.device != codes.device):
         raise ValueError("codes, offsets and values must be on one device")
+    if stream is not None:
+        _check_stream(stream, codes.device)
+        with torch.cuda.stream(stream):
+            return adamw_unpack(codes, offset, signed, values)
     if values is None:
         values = torch.empty(codes.shape, dtype=torch.bfloat16, device=codes.device)
     elif values.dtype != torch.bfloat16 or values.numel() != n:
         raise ValueError("values must hold %d bfloat16 elements" % n)
     with _on(codes.device):
         _check(lib().dropit_adamw_unpack(codes.data_ptr(), offset.data_ptr(), n, 1 if signed else 0, values.data_ptr(),
-                                         _stream_ptr(stream, codes.device)))
+                                         _stream_ptr(None, codes.device)))
     return values
 
 
@@ -279,17 +299,19 @@ def grad_norm(grads: Sequence[torch.Tensor], max_norm: float = math.inf, out: Op
     if g.type == -2 and not set(np.frombuffer(g.types, dtype=np.int32).tolist()) <= {F32, BF16}:
         raise TypeError("dropit supports float32 and bfloat16 tensors, got %s" % sorted({str(t.dtype) for t in grads}))
     where = grads[0].device
+    if stream is not None:
+        _check_stream(stream, where)
+        with torch.cuda.stream(stream):
+            return grad_norm(grads, max_norm, out, workspace)
     if out is None:
         out = torch.empty(2, dtype=torch.float32, device=where)
     elif out.dtype != torch.float32 or out.numel() < 2 or out.get_device() != device or not out.is_contiguous():
         raise ValueError("out must hold two contiguous float32 elements on the gradients' device")
     need = int(lib().dropit_grad_norm_workspace_bytes(g.numels, count))      # (bytes arrive as pointers to them)
-    if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=where) if need else None
-    else:
-        _require_device(workspace)
+    if workspace is not None:
+        _check_tensors(out, workspace)
+    area, size = _area(workspace, need, where)
     with _on(where):
         _check(lib().dropit_grad_norm(g.pointers, g.numels, g.types, count, float(max_norm),
-                                      out.data_ptr(), workspace.data_ptr() if workspace is not None else None,
-                                      workspace.numel() if workspace is not None else 0, _stream_ptr(stream, where)))
+                                      out.data_ptr(), area, size, _stream_ptr(None, where)))
     return out

@@ -27,6 +27,10 @@ def _memory_order(t: torch.Tensor) -> torch.Tensor:
     return v
 
 
+def _same_layout(a: torch.Tensor, b: torch.Tensor) -> bool:
+    return a.stride() == b.stride() or (a.is_contiguous() and b.is_contiguous())
+
+
 def _contiguous(tensors: List[torch.Tensor]) -> bool:
     return layers._marshal().describe(tensors)[5]
 
@@ -70,6 +74,8 @@ class AdamW(torch.optim.Optimizer):
                 raise ValueError("lr, eps and weight_decay must not be negative, betas in [0, 1)")
             if group["state_bits"] not in (8, 32):
                 raise ValueError("state_bits must be 8 or 32, got %r" % (group["state_bits"],))
+            if len(set(map(id, group["params"]))) != len(group["params"]):
+                raise ValueError("a parameter appears twice in a group")
             for p in group["params"]:
                 if p.dtype not in _DTYPES:
                     raise TypeError("AdamW takes float32 and bfloat16 parameters, got %s" % p.dtype)
@@ -107,11 +113,17 @@ class AdamW(torch.optim.Optimizer):
         return out[0], out[1]
 
     def load_state_dict(self, state_dict: Dict[str, Any]) -> None:
-        super().load_state_dict(state_dict)            # (casts floating states to their parameter's type)
         saved = state_dict["state"]
         ids = [i for g in state_dict["param_groups"] for i in g["params"]]
+        own_params = [p for g in self.param_groups for p in g["params"]]
+        for i, p in zip(ids, own_params):
+            state = saved.get(i, {})
+            if "exp_avg_offset" in state and state["exp_avg"].shape == p.shape and not _same_layout(state["exp_avg"], p):
+                raise ValueError("8-bit states go by the order of their parameter in memory: saved with strides %s, loaded with %s"
+                                 % (tuple(state["exp_avg"].stride()), tuple(p.stride())))
+        super().load_state_dict(state_dict)            # (casts floating states to their parameter's type)
         shared: Dict[int, torch.Tensor] = {}           # step counters of capturable groups stay one tensor
-        for i, p in zip(ids, (p for g in self.param_groups for p in g["params"])):
+        for i, p in zip(ids, own_params):
             for name, value in saved.get(i, {}).items():
                 if not isinstance(value, torch.Tensor):
                     self.state[p][name] = value
@@ -146,12 +158,20 @@ class AdamW(torch.optim.Optimizer):
                 if len(params) != len(group["params"]):
                     raise RuntimeError("a capturable group steps together: %d of its %d parameters have no gradient"
                                        % (len(group["params"]) - len(params), len(group["params"])))
-                count = next((s["step"] for s in states if s), None)
-                if count is None:
-                    count = torch.zeros(1, dtype=torch.int32, device=params[0].device)
+                count = next((s["step"] for s in states if s), 0)
+                if not isinstance(count, torch.Tensor):        # (a new group, or one that was not capturable before)
+                    if any(s and s["step"] != count for s in states):
+                        raise RuntimeError("the parameters of a capturable group must have made the same number of steps")
+                    if torch.cuda.is_current_stream_capturing():
+                        raise RuntimeError("AdamW's states are made by its first step: take one outside the capture")
+                    count = torch.full((1,), count, dtype=torch.int32, device=params[0].device)
+                    for s in states:
+                        if s:
+                            s["step"] = count
                 for p, s in zip(params, states):
                     if not s:
                         s.update(self._new_state(p, group, count))
+                self._check_layouts(params, states)
                 work.append((group, count, params, grads, states))
                 continue
             if torch.cuda.is_current_stream_capturing():
@@ -159,6 +179,9 @@ class AdamW(torch.optim.Optimizer):
             for p, s in zip(params, states):
                 if not s:
                     s.update(self._new_state(p, group, 0))
+                elif isinstance(s["step"], torch.Tensor):      # (the group was capturable before)
+                    s["step"] = int(s["step"].item())
+            self._check_layouts(params, states)
             counts = [s["step"] for s in states]
             for t in sorted(set(counts)):
                 at = [j for j, c in enumerate(counts) if c == t]
@@ -187,6 +210,13 @@ class AdamW(torch.optim.Optimizer):
         return loss
 
     @staticmethod
+    def _check_layouts(params, states) -> None:
+        """Moments and residuals go by their parameter's order in memory; all of a state are made alike."""
+        own = [s["exp_avg"] for s in states]
+        if not (_contiguous(params) and _contiguous(own)) and not all(map(_same_layout, own, params)):
+            raise RuntimeError("a parameter's strides have changed since its states were made")
+
+    @staticmethod
     def _grad(p: torch.Tensor, g: torch.Tensor) -> torch.Tensor:
         if g.stride() != p.stride() and not (g.is_contiguous() and p.is_contiguous()):
             g = torch.empty_like(p, dtype=g.dtype, memory_format=torch.preserve_format).copy_(g)
@@ -201,3 +231,4 @@ class AdamW(torch.optim.Optimizer):
             more["residual"] = column("residual")
         layers.adamw(_all_in_memory_order(params), _all_in_memory_order(grads), column("exp_avg"), column("exp_avg_sq"), lr=group["lr"],
                      betas=group["betas"], eps=group["eps"], weight_decay=group["weight_decay"], step=t, grad_scale=scale, **more)
+        torch.autograd.graph.increment_version(params)  # (a graph that saved them must not go backward with the new values)

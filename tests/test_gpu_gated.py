@@ -249,6 +249,28 @@ def test_leading_dimensions_empty_batches_and_streams():
     assert torch.equal(late, h)
 
 
+def test_what_a_call_allocates_belongs_to_its_stream():
+    print("gated allocation", flush=True)
+    x, w, b, dh = (t.to(DEV) for t in inputs(600, 264, 520, "bf16", True, 12))
+    h, pre = dropit.gated_forward(x, w, b, save=True)
+    back = dropit.gated_backward(dh, pre, w, need_dbias=True)
+    norm = dropit.grad_norm([x, w])
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    # memory that the current stream will still write: freed here, it may serve this stream, not another
+    doomed = [torch.empty(n, dtype=torch.uint8, device=DEV) for n in (600 * 520 * 2, 600 * 1040 * 2, 600 * 264 * 2, 2 << 20, 4096, 512)]
+    torch.cuda._sleep(20_000_000)
+    for d in doomed:
+        d.fill_(255)
+    del doomed, d
+    got = dropit.gated_forward(x, w, b, save=True, stream=side)
+    got_back = dropit.gated_backward(dh, pre, w, need_dbias=True, stream=side)
+    got_norm = dropit.grad_norm([x, w], stream=side)
+    torch.cuda.synchronize()
+    for mine, other in zip((h, pre) + back + (norm,), got + got_back + (got_norm,)):
+        assert torch.equal(mine, other)
+
+
 @pytest.mark.parametrize("tokens,c,hidden,dtype", [(3, 512, 64, "bf16"), (40, 512, 48, "f32"), (600, 264, 520, "bf16")])
 def test_graph_replays_follow_their_inputs(tokens, c, hidden, dtype):
     print("gated graph", tokens, c, hidden, dtype, flush=True)

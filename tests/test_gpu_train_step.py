@@ -277,6 +277,70 @@ def test_capture_is_refused_where_a_replay_would_be_wrong():
         both.step()
 
 
+def test_a_saved_parameter_does_not_go_backward_after_the_step():
+    print("optim version", flush=True)
+    p = torch.nn.Parameter(torch.randn(300, device=DEV))
+    p.grad = torch.ones(300, device=DEV)
+    loss = (p * p).sum()
+    dropit.optim.AdamW([p]).step()
+    with pytest.raises(RuntimeError, match="inplace"):
+        loss.backward()
+
+
+def test_states_stay_with_their_elements_when_a_layout_changes():
+    print("optim layout change", flush=True)
+    for bits in (8, 32):
+        p = torch.nn.Parameter(torch.randn(8, 6, 5, 5, device=DEV))
+        opt = dropit.optim.AdamW([p], state_bits=bits)
+        p.grad = torch.randn_like(p)
+        opt.step()
+        saved = opt.state_dict()
+        p.data = p.data.to(memory_format=torch.channels_last)
+        p.grad = torch.randn_like(p)
+        with pytest.raises(RuntimeError, match="strides have changed"):
+            opt.step()
+        assert opt.state[p]["step"] == 1
+        other = dropit.optim.AdamW([p], state_bits=bits)
+        if bits == 8:
+            with pytest.raises(ValueError, match="order of their parameter"):
+                other.load_state_dict(saved)
+        else:
+            other.load_state_dict(saved)
+            assert other.state[p]["exp_avg"].stride() == p.stride() and torch.equal(other.state[p]["exp_avg"], opt.state[p]["exp_avg"])
+            other.step()
+
+
+def test_a_group_becomes_capturable_and_back():
+    print("optim capturable on and off", flush=True)
+    p, q = (torch.nn.Parameter(torch.ones(700, device=DEV)) for _ in range(2))
+    a, b = dropit.optim.AdamW([p]), dropit.optim.AdamW([q])
+    for t in range(6):
+        p.grad = torch.randn(700, device=DEV)
+        q.grad = p.grad.clone()
+        a.param_groups[0]["capturable"] = t in (2, 3)
+        a.step()
+        b.step()
+        # the count's corrections are the host's double pow or the device's repeated squaring, rounded to fp32 each: a step of
+        # 2^-24 of two factors of an update of about lr
+        assert int(a.state[p]["step"]) == t + 1
+        assert float((p - q).detach().abs().max()) <= (t + 1) * (4 * 2.0 ** -24 * 1.1e-3 + 2.0 ** -24)
+
+
+def test_gradients_of_odd_rows_that_start_anywhere():
+    print("gated narrow gradient", flush=True)
+    torch.manual_seed(3)
+    x = torch.randn(5, 64, device=DEV)
+    layer = dropit.nn.GatedLinear(64, 33, gamma=0.0, device=DEV)
+    h = layer(x)
+    head = torch.randn(1, 33, device=DEV, requires_grad=True)
+    weights = torch.randn(6, 33, device=DEV)
+    (torch.cat([head, h]) * weights).sum().backward()              # h's gradient starts 132 bytes into another's storage
+    got = layer.weight.grad.clone()
+    layer.weight.grad = None
+    (layer(x) * weights[1:]).sum().backward()
+    assert torch.equal(layer.weight.grad, got)
+
+
 def test_block_bench_runs_with_the_gated_block_and_adamw():
     print("block bench", flush=True)
     import argparse

@@ -58,6 +58,8 @@ def test_adamw_refuses_bad_arguments():
     for bad in (torch.zeros(4, dtype=torch.float16), torch.zeros(4, dtype=torch.float64), torch.zeros(8)[::2], torch.zeros(4, 1).expand(4, 3)):
         with pytest.raises(TypeError):
             dropit.optim.AdamW([torch.nn.Parameter(bad)])
+    with pytest.raises(ValueError, match="twice"):
+        dropit.optim.AdamW([p, p])
     opt = dropit.optim.AdamW([p])
     opt.step()                                         # no gradients: nothing to do
     p.grad = torch.ones(4)
