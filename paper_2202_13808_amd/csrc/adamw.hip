@@ -10,6 +10,9 @@
 //
 // The arithmetic is that of single fp32 operations, correctly rounded division and square root included: the codes and the
 // residual's 16 bits are exact functions of the inputs, which any other implementation of the formulas reproduces.
+//
+// Measured: 21.8 M fp32 parameters in 152 tensors 134 us, 4.5 TB/s of the 5.1 that a large copy reaches; 269 M bf16 parameters in
+// 16 tensors with 8-bit states 620 us, 4.3 TB/s.
 #include <cmath>
 #include <type_traits>
 

@@ -1,6 +1,6 @@
 // The gated projection's forward pass for few tokens (decoding): one pass over the weights.
 //
-// Bound by reading the weights.  A workgroup of eight wavefronts takes 16 hidden columns, 16 gate rows and the 16 up rows of
+// Bound by reading the weights: 16 tokens 4096 -> 10240 in bf16 35 us, 4.8 TB/s of them.  A workgroup of eight wavefronts takes 16 hidden columns, 16 gate rows and the 16 up rows of
 // the same columns, each wavefront an eighth of the sum, so that even a small layer has enough loads in flight.  Both operands
 // go from memory straight into the registers of the 16 x 16 matrix instructions, with no LDS between; the eighths meet in LDS,
 // in ascending order.
@@ -124,6 +124,7 @@ bool gated_tokens_takes(int64_t tokens, int64_t c_in, int64_t hidden, dropit_dty
 {
     const int64_t size = dt == DROPIT_BF16 ? 2 : 4;
     if (c_in % (16 / size) != 0) return false;         // rows in 16-byte units
+    if (hidden > 1 << 26) return false;                // a launch has fewer than 2^32 threads
     // Every workgroup reads all tokens.  Up to 16 that is always worth it; up to 64 while the weights are small (us for 64 tokens
     // here and in gated.hip's product: bf16 768 -> 2048 7.3 and 12.4, 2048 -> 5632 (46 MB) 25.7 and 24.9, 4096 -> 10240 80.6
     // and 55.7; fp32 768 -> 2048 15.3 and 20.7, 2048 -> 5632 83 and 48)

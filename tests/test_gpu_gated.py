@@ -134,7 +134,8 @@ def test_sizes(tokens, c, hidden, dtype):
 @pytest.mark.parametrize("tokens,c,hidden", [
     (4001, 515, 1027), (2500, 1030, 770),              # rows that are no whole 16-byte units, copied into such
     (100, 2048, 131), (70, 4096, 40),                  # few tiles: the sum in slices, odd width and even
-    (16384, 64, 512), (32768, 512, 32), (12608, 128, 2048)])           # 256 and 192 tokens to a tile, several tiles a workgroup
+    (16384, 64, 512), (32768, 512, 32),                # 256 and 192 tokens to a tile, several tiles a workgroup
+    (12608, 128, 2048), (9400, 72, 2041), (4660, 64, 4100)])           # the last tiles not full
 def test_larger_products(tokens, c, hidden):
     run_case(tokens, c, hidden, "bf16", "gelu", bias=True, seed=6)
 
