@@ -33,7 +33,7 @@ extern "C" {
  *
  * x [tokens, c_in], w, bias, h, pre: device, row-major, type dt, 16-byte aligned; pre may be NULL (inference).
  * 0 <= tokens < 2^31, 1 <= c_in <= 2^28, 1 <= hidden <= 2^27, and ceil(tokens / 64) times the larger of ceil(hidden / 32) and
- * ceil(c_in / 64) less than 2^24.  Row offsets are 64-bit: none of the tensors is limited to 2^31 elements.
+ * ceil(c_in / 64) at most 2^24 - 8.  Row offsets are 64-bit: none of the tensors is limited to 2^31 elements.
  */
 typedef DROPIT_ENUM(dropit_act) {
     DROPIT_ACT_SILU = 0,
