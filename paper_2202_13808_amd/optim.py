@@ -46,7 +46,7 @@ class AdamW(torch.optim.Optimizer):
     ``residual``    bfloat16 parameters keep 16 more bits each and follow their fp32 values exactly (default); False rounds
                     them to bfloat16 every step, which loses updates of less than a 256th of a parameter
     ``max_norm``    the gradients' global 2-norm, over all groups, is clipped to this (None: not); ``last_grad_norm`` is then
-                    the unclipped norm, a device scalar
+                    the unclipped norm, a device scalar.  Copies of the optimizer keep both; ``state_dict()`` holds neither
     ``capturable``  the step count lives on the device, so that ``step()`` can be captured into a HIP graph and replayed.  All
                     parameters of a group then step together: a missing gradient is an error.  Take one step outside the
                     capture first (it makes the states).  ``lr`` and the other numbers are captured as they are.
@@ -62,6 +62,10 @@ class AdamW(torch.optim.Optimizer):
         self.last_grad_norm: Optional[torch.Tensor] = None
         super().__init__(params, dict(lr=lr, betas=betas, eps=eps, weight_decay=weight_decay, state_bits=state_bits,
                                       residual=bool(residual), capturable=bool(capturable)))
+
+    def __getstate__(self) -> Dict[str, Any]:
+        # (copies and pickles carry what this says; torch's names the groups and the states only)
+        return {**super().__getstate__(), "max_norm": self.max_norm, "last_grad_norm": self.last_grad_norm}
 
     def add_param_group(self, param_group: Dict[str, Any]) -> None:
         super().add_param_group(param_group)
