@@ -117,18 +117,41 @@ class AdamW(torch.optim.Optimizer):
         return out[0], out[1]
 
     def load_state_dict(self, state_dict: Dict[str, Any]) -> None:
-        saved = state_dict["state"]
+        """Loads what the pre-hooks make of ``state_dict``; the post-hooks find the states as they stay."""
+        loaded: Dict[str, Any] = {}
+
+        def behind_the_pre_hooks(_, sd: Dict[str, Any]) -> None:
+            loaded.update(sd)
+            for p, state in self._states_of(loaded):
+                self._check_loaded(p, state)
+
+        def before_the_post_hooks(_) -> None:
+            self._take_states(loaded)
+
+        handles = (self.register_load_state_dict_pre_hook(behind_the_pre_hooks),
+                   self.register_load_state_dict_post_hook(before_the_post_hooks, prepend=True))
+        try:
+            super().load_state_dict(state_dict)
+        finally:
+            for handle in handles:
+                handle.remove()
+
+    def _states_of(self, state_dict: Dict[str, Any]) -> List[Tuple[torch.Tensor, Dict[str, Any]]]:
         ids = [i for g in state_dict["param_groups"] for i in g["params"]]
-        own_params = [p for g in self.param_groups for p in g["params"]]
-        for i, p in zip(ids, own_params):
-            state = saved.get(i, {})
-            if "exp_avg_offset" in state and state["exp_avg"].shape == p.shape and not _same_layout(state["exp_avg"], p):
-                raise ValueError("8-bit states go by the order of their parameter in memory: saved with strides %s, loaded with %s"
-                                 % (tuple(state["exp_avg"].stride()), tuple(p.stride())))
-        super().load_state_dict(state_dict)            # (casts floating states to their parameter's type)
+        own = [p for g in self.param_groups for p in g["params"]]
+        return [(p, state_dict["state"].get(i, {})) for i, p in zip(ids, own)]
+
+    @staticmethod
+    def _check_loaded(p: torch.Tensor, state: Dict[str, Any]) -> None:
+        if "exp_avg_offset" in state and state["exp_avg"].shape == p.shape and not _same_layout(state["exp_avg"], p):
+            raise ValueError("8-bit states go by the order of their parameter in memory: saved with strides %s, loaded with %s"
+                             % (tuple(state["exp_avg"].stride()), tuple(p.stride())))
+
+    def _take_states(self, state_dict: Dict[str, Any]) -> None:
+        """The loaded states in their own types (torch's loading casts floating ones to their parameter's)."""
         shared: Dict[int, torch.Tensor] = {}           # step counters of capturable groups stay one tensor
-        for i, p in zip(ids, own_params):
-            for name, value in saved.get(i, {}).items():
+        for p, state in self._states_of(state_dict):
+            for name, value in state.items():
                 if not isinstance(value, torch.Tensor):
                     self.state[p][name] = value
                 elif name == "step":

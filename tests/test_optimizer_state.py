@@ -28,3 +28,60 @@ def test_loading_a_state_keeps_the_own_clipping():
     a, b = dropit.optim.AdamW([p], max_norm=0.5), dropit.optim.AdamW([q], max_norm=2.0)
     a.load_state_dict(b.state_dict())
     assert a.max_norm == 0.5 and a.last_grad_norm is None
+
+
+def _saved(p, value, step=3, bits=32, **group):
+    """A state dictionary of one parameter whose first moment is `value` throughout."""
+    opt = dropit.optim.AdamW([p], state_bits=bits, **group)
+    moment = lambda x: torch.full_like(p, x, dtype=torch.float32 if bits == 32 else torch.uint8)  # noqa: E731
+    state = {"step": step, "exp_avg": moment(value), "exp_avg_sq": moment(1)}
+    if bits == 8:
+        for name in ("exp_avg_offset", "exp_avg_sq_offset"):
+            state[name] = torch.zeros((p.numel() + 255) // 256, dtype=torch.int16)
+    if p.dtype == torch.bfloat16 and opt.param_groups[0]["residual"]:
+        state["residual"] = torch.zeros_like(p, dtype=torch.int16)
+    opt.state[p].update(state)
+    return opt.state_dict()
+
+
+def test_what_a_pre_hook_returns_is_loaded():
+    p = torch.nn.Parameter(torch.zeros(5, dtype=torch.bfloat16))
+    opt = dropit.optim.AdamW([p])
+    other = _saved(torch.nn.Parameter(torch.zeros(5, dtype=torch.bfloat16)), 1.0009765625, step=9)
+    opt.register_load_state_dict_pre_hook(lambda o, sd: other)
+    opt.load_state_dict(_saved(p, 7.0))
+    # (a value that bfloat16 does not hold: the moments stay in their own type)
+    assert opt.state[p]["exp_avg"].dtype == torch.float32 and bool((opt.state[p]["exp_avg"] == 1.0009765625).all())
+    assert opt.state[p]["step"] == 9
+
+
+def test_a_post_hook_has_the_last_word():
+    p = torch.nn.Parameter(torch.zeros(5, dtype=torch.bfloat16))
+    opt = dropit.optim.AdamW([p])
+    seen = []
+
+    def change(o):
+        seen.append(o.state[p]["exp_avg"].clone())
+        o.state[p]["exp_avg"].fill_(2.0)
+        o.state[p]["step"] = 50
+
+    handle = opt.register_load_state_dict_post_hook(change)
+    opt.load_state_dict(_saved(p, 1.0009765625))
+    assert seen[0].dtype == torch.float32 and bool((seen[0] == 1.0009765625).all())
+    assert bool((opt.state[p]["exp_avg"] == 2.0).all()) and opt.state[p]["step"] == 50
+    handle.remove()
+    opt.load_state_dict(_saved(p, 4.0))                # nothing of the first call stays behind
+    assert bool((opt.state[p]["exp_avg"] == 4.0).all()) and opt.state[p]["step"] == 3
+
+
+def test_a_layout_that_codes_do_not_fit_is_refused_whatever_hook_brought_it():
+    p = torch.nn.Parameter(torch.zeros(2, 3, 4, 4).to(memory_format=torch.channels_last))
+    opt = dropit.optim.AdamW([p], state_bits=8)
+    plain = _saved(torch.nn.Parameter(torch.zeros(2, 3, 4, 4)), 1, bits=8)
+    before = copy.deepcopy(opt.state_dict())
+    handle = opt.register_load_state_dict_pre_hook(lambda o, sd: plain)
+    with pytest.raises(ValueError, match="order of their parameter"):
+        opt.load_state_dict(before)
+    assert opt.state_dict() == before
+    handle.remove()
+    opt.load_state_dict(before)
