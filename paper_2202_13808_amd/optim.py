@@ -14,6 +14,7 @@ import torch
 from . import layers
 
 _DTYPES = (torch.float32, torch.bfloat16)
+_GROUP_KEYS = ("lr", "betas", "eps", "weight_decay", "state_bits", "residual", "capturable")
 
 
 def _memory_order(t: torch.Tensor) -> torch.Tensor:
@@ -117,13 +118,16 @@ class AdamW(torch.optim.Optimizer):
         return out[0], out[1]
 
     def load_state_dict(self, state_dict: Dict[str, Any]) -> None:
-        """Loads what the pre-hooks make of ``state_dict``; the post-hooks find the states as they stay."""
+        """Loads what the pre-hooks make of ``state_dict``; the post-hooks find the states as they stay.  What does not fit the
+        parameters (another optimizer's states, other types or sizes) is refused and changes nothing."""
         loaded: Dict[str, Any] = {}
 
         def behind_the_pre_hooks(_, sd: Dict[str, Any]) -> None:
             loaded.update(sd)
-            for p, state in self._states_of(loaded):
-                self._check_loaded(p, state)
+            for group in sd["param_groups"]:
+                self._check_loaded_group(group)
+            for p, group, state in self._states_of(loaded):
+                self._check_loaded(p, group, state)
 
         def before_the_post_hooks(_) -> None:
             self._take_states(loaded)
@@ -136,21 +140,51 @@ class AdamW(torch.optim.Optimizer):
             for handle in handles:
                 handle.remove()
 
-    def _states_of(self, state_dict: Dict[str, Any]) -> List[Tuple[torch.Tensor, Dict[str, Any]]]:
-        ids = [i for g in state_dict["param_groups"] for i in g["params"]]
+    def _states_of(self, state_dict: Dict[str, Any]) -> List[Tuple[torch.Tensor, Dict[str, Any], Dict[str, Any]]]:
+        """Parameter, saved group and saved state of every parameter."""
+        saved = [(i, g) for g in state_dict["param_groups"] for i in g["params"]]
         own = [p for g in self.param_groups for p in g["params"]]
-        return [(p, state_dict["state"].get(i, {})) for i, p in zip(ids, own)]
+        return [(p, g, state_dict["state"].get(i, {})) for (i, g), p in zip(saved, own)]
 
     @staticmethod
-    def _check_loaded(p: torch.Tensor, state: Dict[str, Any]) -> None:
-        if "exp_avg_offset" in state and state["exp_avg"].shape == p.shape and not _same_layout(state["exp_avg"], p):
+    def _check_loaded_group(group: Dict[str, Any]) -> None:
+        missing = [k for k in _GROUP_KEYS if k not in group]
+        if missing:
+            raise ValueError("not a group of this optimizer: it lacks %s (a load_state_dict pre-hook can turn another's states into its)"
+                             % ", ".join(missing))
+        if group["state_bits"] not in (8, 32):
+            raise ValueError("state_bits must be 8 or 32, got %r" % (group["state_bits"],))
+
+    @staticmethod
+    def _check_loaded(p: torch.Tensor, group: Dict[str, Any], state: Dict[str, Any]) -> None:
+        if not state:                                  # (no step yet)
+            return
+        bits8 = group["state_bits"] == 8
+        moment = (torch.uint8 if bits8 else torch.float32, p.numel())
+        kinds = {"exp_avg": moment, "exp_avg_sq": moment}
+        if bits8:
+            kinds["exp_avg_offset"] = kinds["exp_avg_sq_offset"] = (torch.int16, (p.numel() + layers.ADAMW_BLOCK - 1) // layers.ADAMW_BLOCK)
+        if "residual" in state:
+            if p.dtype != torch.bfloat16:
+                raise ValueError("a state with a residual belongs to a bfloat16 parameter, not to one of %s" % p.dtype)
+            kinds["residual"] = (torch.int16, p.numel())
+        for name, (dtype, numel) in kinds.items():
+            value = state.get(name)
+            if not isinstance(value, torch.Tensor) or value.dtype != dtype or value.numel() != numel:
+                raise ValueError("%s of a parameter of shape %s in %d-bit states must be %d elements of %s" % (
+                    name, tuple(p.shape), group["state_bits"], numel, dtype))
+        step = state.get("step", -1)
+        step = step.item() if isinstance(step, torch.Tensor) and step.numel() == 1 else step
+        if isinstance(step, torch.Tensor) or step != int(step) or step < 0:
+            raise ValueError("a state's step must be a count, got %r" % (state.get("step"),))
+        if bits8 and state["exp_avg"].shape == p.shape and not _same_layout(state["exp_avg"], p):
             raise ValueError("8-bit states go by the order of their parameter in memory: saved with strides %s, loaded with %s"
                              % (tuple(state["exp_avg"].stride()), tuple(p.stride())))
 
     def _take_states(self, state_dict: Dict[str, Any]) -> None:
         """The loaded states in their own types (torch's loading casts floating ones to their parameter's)."""
         shared: Dict[int, torch.Tensor] = {}           # step counters of capturable groups stay one tensor
-        for p, state in self._states_of(state_dict):
+        for p, group, state in self._states_of(state_dict):
             for name, value in state.items():
                 if not isinstance(value, torch.Tensor):
                     self.state[p][name] = value
@@ -160,6 +194,9 @@ class AdamW(torch.optim.Optimizer):
                     own = torch.empty_like(p, dtype=value.dtype, memory_format=torch.preserve_format) if value.shape == p.shape \
                         else torch.empty(value.shape, dtype=value.dtype, device=p.device)
                     self.state[p][name] = own.copy_(value)
+            if state and group["residual"] and p.dtype == torch.bfloat16 and "residual" not in state:
+                # (saved of an fp32 parameter: the bf16 value as it is)
+                self.state[p]["residual"] = torch.zeros_like(p, dtype=torch.int16, memory_format=torch.preserve_format)
 
     # ---- the step --------------------------------------------------------------------------------
     @torch.no_grad()

@@ -85,3 +85,75 @@ def test_a_layout_that_codes_do_not_fit_is_refused_whatever_hook_brought_it():
     assert opt.state_dict() == before
     handle.remove()
     opt.load_state_dict(before)
+
+
+def test_states_of_another_optimizer_are_refused_when_they_are_loaded():
+    p = torch.nn.Parameter(torch.zeros(300))
+    p.grad = torch.ones(300)
+    other = torch.optim.AdamW([p])
+    fresh = other.state_dict()
+    other.step()
+    opt = dropit.optim.AdamW([p])
+    before = opt.state_dict()
+    for foreign in (fresh, other.state_dict()):
+        with pytest.raises(ValueError, match="state_bits"):
+            opt.load_state_dict(foreign)
+        assert opt.state_dict() == before
+    # a hook that turns the one into the other makes it loadable
+    keys = {k: v for k, v in before["param_groups"][0].items() if k != "params"}
+
+    def adapt(o, sd):
+        groups = [{**keys, **{k: v for k, v in g.items() if k in keys or k == "params"}} for g in sd["param_groups"]]
+        return {"state": {i: {**s, "step": int(s["step"])} for i, s in sd["state"].items()}, "param_groups": groups}
+
+    opt.register_load_state_dict_pre_hook(adapt)
+    opt.load_state_dict(other.state_dict())
+    assert opt.state[p]["step"] == 1 and torch.equal(opt.state[p]["exp_avg"], other.state[p]["exp_avg"])
+    assert opt.param_groups[0]["state_bits"] == 32
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("bits", [8, 32])
+def test_states_that_do_not_fit_their_parameter_or_group_are_refused_when_they_are_loaded(bits, dtype):
+    p = torch.nn.Parameter(torch.zeros(300, dtype=dtype))
+    good = _saved(p, 1, bits=bits)
+    opt = dropit.optim.AdamW([p], state_bits=bits)
+    opt.load_state_dict(good)
+    bad = [{"exp_avg": torch.zeros(299)}, {"exp_avg_sq": torch.zeros(300, dtype=torch.float64)},
+           {"exp_avg": torch.zeros(300, dtype=torch.bfloat16)}, {"step": 2.5}, {"step": -1}]
+    if bits == 8:
+        bad += [{"exp_avg_offset": torch.zeros(1, dtype=torch.int16)}, {"exp_avg_sq_offset": torch.zeros(2, dtype=torch.int32)}]
+    if dtype == torch.bfloat16:
+        bad += [{"residual": torch.zeros(300)}, {"residual": torch.zeros(10, dtype=torch.int16)}]
+    else:
+        bad += [{"residual": torch.zeros(300, dtype=torch.int16)}]
+    for change in bad:
+        sd = copy.deepcopy(good)
+        sd["state"][0].update(change)
+        with pytest.raises(ValueError):
+            opt.load_state_dict(sd)
+    for missing in set(good["state"][0]) - {"residual"}:
+        sd = copy.deepcopy(good)
+        del sd["state"][0][missing]
+        with pytest.raises(ValueError):
+            opt.load_state_dict(sd)
+    sd = copy.deepcopy(good)
+    sd["param_groups"][0]["state_bits"] = 40 - bits    # a group says what its states are
+    with pytest.raises(ValueError):
+        opt.load_state_dict(sd)
+    assert opt.param_groups[0]["state_bits"] == bits and opt.state[p]["step"] == 3
+    for name, value in good["state"][0].items():
+        assert torch.equal(torch.as_tensor(opt.state[p][name]), torch.as_tensor(value))
+    # a parameter that has made no step has no state
+    sd = copy.deepcopy(good)
+    sd["state"] = {}
+    opt.load_state_dict(sd)
+    assert not opt.state[p]
+
+
+def test_states_of_float32_parameters_loaded_for_bfloat16_ones_start_without_residuals():
+    p, q = torch.nn.Parameter(torch.zeros(300)), torch.nn.Parameter(torch.zeros(300, dtype=torch.bfloat16))
+    opt = dropit.optim.AdamW([q])
+    opt.load_state_dict(_saved(p, 1.5))
+    assert opt.state[q]["exp_avg"].dtype == torch.float32 and bool((opt.state[q]["exp_avg"] == 1.5).all())
+    assert opt.state[q]["residual"].dtype == torch.int16 and not bool(opt.state[q]["residual"].any())
