@@ -128,6 +128,9 @@ class AdamW(torch.optim.Optimizer):
                 self._check_loaded_group(group)
             for p, group, state in self._states_of(loaded):
                 self._check_loaded(p, group, state)
+            for group in sd["param_groups"]:
+                if group["capturable"] and len({int(sd["state"][i]["step"]) for i in group["params"] if sd["state"].get(i)}) > 1:
+                    raise ValueError("the parameters of a capturable group must have made the same number of steps")
 
         def before_the_post_hooks(_) -> None:
             self._take_states(loaded)
@@ -183,13 +186,16 @@ class AdamW(torch.optim.Optimizer):
 
     def _take_states(self, state_dict: Dict[str, Any]) -> None:
         """The loaded states in their own types (torch's loading casts floating ones to their parameter's)."""
-        shared: Dict[int, torch.Tensor] = {}           # step counters of capturable groups stay one tensor
+        counts: Dict[int, torch.Tensor] = {}           # a capturable group's parameters share one, which its step raises
         for p, group, state in self._states_of(state_dict):
             for name, value in state.items():
-                if not isinstance(value, torch.Tensor):
+                if name == "step":
+                    count: Any = int(value)
+                    if group["capturable"]:
+                        count = counts.setdefault(id(group), torch.full((1,), count, dtype=torch.int32, device=p.device))
+                    self.state[p][name] = count
+                elif not isinstance(value, torch.Tensor):
                     self.state[p][name] = value
-                elif name == "step":
-                    self.state[p][name] = shared.setdefault(id(value), value.to(p.device, copy=True))
                 else:
                     own = torch.empty_like(p, dtype=value.dtype, memory_format=torch.preserve_format) if value.shape == p.shape \
                         else torch.empty(value.shape, dtype=value.dtype, device=p.device)

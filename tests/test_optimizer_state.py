@@ -157,3 +157,26 @@ def test_states_of_float32_parameters_loaded_for_bfloat16_ones_start_without_res
     opt.load_state_dict(_saved(p, 1.5))
     assert opt.state[q]["exp_avg"].dtype == torch.float32 and bool((opt.state[q]["exp_avg"] == 1.5).all())
     assert opt.state[q]["residual"].dtype == torch.int16 and not bool(opt.state[q]["residual"].any())
+
+
+def test_counts_loaded_for_a_capturable_group_are_one_tensor():
+    params = [torch.nn.Parameter(torch.zeros(4)) for _ in range(3)]
+
+    def saved(*counts):                                # as they arrive when each tensor was moved by itself
+        parts = [_saved(p, 1.0, step=torch.full((1,), c, dtype=torch.int32), capturable=True)["state"][0] for p, c in zip(params, counts)]
+        groups = dropit.optim.AdamW(params, capturable=True).state_dict()["param_groups"]
+        return {"state": dict(enumerate(parts)), "param_groups": groups}
+
+    opt = dropit.optim.AdamW(params, capturable=True)
+    opt.load_state_dict(saved(7, 7, 7))
+    counts = [opt.state[p]["step"] for p in params]
+    assert counts[0].dtype == torch.int32 and counts[0].tolist() == [7]
+    assert counts[1] is counts[0] and counts[2] is counts[0]       # a step counts them all
+    with pytest.raises(ValueError, match="same number of steps"):
+        opt.load_state_dict(saved(7, 7, 8))
+    assert counts[0].tolist() == [7] and opt.state[params[2]]["step"] is counts[0]
+    # a group that is not capturable counts on the host, each parameter for itself
+    sd = saved(7, 9, 8)
+    sd["param_groups"][0]["capturable"] = False
+    opt.load_state_dict(sd)
+    assert [opt.state[p]["step"] for p in params] == [7, 9, 8] and type(opt.state[params[0]]["step"]) is int
