@@ -41,7 +41,8 @@ def _all_in_memory_order(tensors: List[torch.Tensor]) -> List[torch.Tensor]:
 
 
 class AdamW(torch.optim.Optimizer):
-    """AdamW with decoupled weight decay over float32 and bfloat16 device parameters.
+    """AdamW with decoupled weight decay over float32 and bfloat16 device parameters.  A group's parameters are on one device;
+    with ``max_norm``, all groups' are.
 
     ``state_bits``  32 (fp32 moments) or 8 (blocks of 256 codes, see ``dropit_adamw``); a group may have its own
     ``residual``    bfloat16 parameters keep 16 more bits each and follow their fp32 values exactly (default); False rounds
@@ -219,8 +220,11 @@ class AdamW(torch.optim.Optimizer):
             if not params:
                 continue
             grads = [g for _, g in pairs if g is not None]
-            if layers._marshal().describe(params)[4] == -1:
+            device = layers._marshal().describe(params)[4]
+            if device == -1:
                 raise RuntimeError("AdamW steps device parameters only: there is no CPU path")
+            if device < 0:
+                raise RuntimeError("the parameters of a group must be on one device: give each device a group of its own")
             if not (_contiguous(params) and _contiguous(grads)):
                 grads = [self._grad(p, g) for p, g in zip(params, grads)]
             states = [self.state[p] for p in params]
