@@ -249,6 +249,18 @@ class _GatedFn(torch.autograd.Function):
         return dx, dw, db.to(ctx.bias_dtype) if db is not None else None, None, None, None, None
 
 
+# Whether torch.func's transforms wrap the tensors of this call; None where torch does not say
+_transforms_active = getattr(torch._C, "_are_functorch_transforms_active", None)
+
+
+def _followed(*tensors: Optional[torch.Tensor]) -> bool:
+    """Whether something other than a backward pass follows the torch operators of a call (forward-mode differentiation, a
+    function transform, a trace): it would not see the library's kernels, and its result would miss them."""
+    if torch.jit.is_tracing() or (_transforms_active is not None and _transforms_active()):
+        return True
+    return any(t is not None and torch.autograd.forward_ad.unpack_dual(t).tangent is not None for t in tensors)
+
+
 def _gated_plain(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor], act: str) -> torch.Tensor:
     gate, up = F.linear(x, weight, bias).chunk(2, -1)
     gate = {"silu": F.silu, "gelu": F.gelu, "gelu_tanh": lambda z: F.gelu(z, approximate="tanh"), "relu": F.relu,
@@ -261,7 +273,9 @@ def gated_linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Ten
     """``act(x Wg^T + bg) * (x Wu^T + bu)`` with ``weight`` = [Wg; Wu] of shape [2 * hidden, c_in] and ``bias`` [2 * hidden]:
     both projections, the activation (silu, gelu, gelu_tanh, relu, sigmoid) and the product in one kernel.  The backward pass
     takes the weight gradient from the min-k cache of ``x`` (``gamma`` = 0 keeps ``x`` itself; ``seed`` and ``index_format``
-    as for ``linear``) and keeps the pre-activations whole.  Under autocast the operands are cast as ``F.linear``'s are."""
+    as for ``linear``) and keeps the pre-activations whole.  Under autocast the operands are cast as ``F.linear``'s are.
+    Where nothing requires a gradient, forward-mode differentiation, ``torch.func`` and ``torch.jit.trace`` get the formula in
+    torch's operators, which they can follow; through the dropping layer they are refused."""
     layers._act_code(act)
     layers._gated_sizes(weight)
     _check_format(index_format)
@@ -274,6 +288,8 @@ def gated_linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Ten
         return _gated_plain(x, weight, bias, act)
     with torch.autocast("cuda", enabled=False):
         if not torch.is_grad_enabled() or not any(t is not None and t.requires_grad for t in (x, weight, bias)):
+            if _followed(x, weight, bias):
+                return _gated_plain(x, weight, bias, act)
             return layers.gated_forward(_contiguous(x), _contiguous(weight), _contiguous(bias) if bias is not None else None, act=act)
         if x.numel() == 0:
             gamma = 0.0
