@@ -249,6 +249,8 @@ class _GatedFn(torch.autograd.Function):
         return dx, dw, db.to(ctx.bias_dtype) if db is not None else None, None, None, None, None
 
 
+_KERNEL_DTYPES = (torch.float32, torch.bfloat16)
+
 # Whether torch.func's transforms wrap the tensors of this call; None where torch does not say
 _transforms_active = getattr(torch._C, "_are_functorch_transforms_active", None)
 
@@ -275,7 +277,8 @@ def gated_linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Ten
     takes the weight gradient from the min-k cache of ``x`` (``gamma`` = 0 keeps ``x`` itself; ``seed`` and ``index_format``
     as for ``linear``) and keeps the pre-activations whole.  Under autocast the operands are cast as ``F.linear``'s are.
     Where nothing requires a gradient, forward-mode differentiation, ``torch.func`` and ``torch.jit.trace`` get the formula in
-    torch's operators, which they can follow; through the dropping layer they are refused."""
+    torch's operators, which they can follow; through the dropping layer they are refused.  Types other than float32 and bfloat16
+    run in torch's operators too where nothing is dropped, and are refused where something is."""
     layers._act_code(act)
     layers._gated_sizes(weight)
     _check_format(index_format)
@@ -287,6 +290,8 @@ def gated_linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Ten
             raise RuntimeError("DropIT layers train on device tensors only: there is no CPU path")
         return _gated_plain(x, weight, bias, act)
     with torch.autocast("cuda", enabled=False):
+        if x.dtype not in _KERNEL_DTYPES and not (gamma > 0.0 and torch.is_grad_enabled() and weight.requires_grad):
+            return _gated_plain(x, weight, bias, act)
         if not torch.is_grad_enabled() or not any(t is not None and t.requires_grad for t in (x, weight, bias)):
             if _followed(x, weight, bias):
                 return _gated_plain(x, weight, bias, act)

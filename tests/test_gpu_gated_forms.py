@@ -77,3 +77,26 @@ def test_a_traced_layer_computes():
         traced = torch.jit.trace(layer, (x,))
         for t in (x, other):
             assert float((traced(t) - layer(t)).abs().max()) <= 64 * 2.0 ** -24 * 10
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.float64])
+def test_types_without_a_kernel_run_plainly_where_nothing_is_dropped(dtype):
+    print("gated other types", dtype, flush=True)
+    wide = _layer("silu").eval()
+    layer = _layer("silu", dtype=dtype, gamma=0.0)
+    x = torch.randn(5, 24, device=DEV)
+    half = torch.finfo(dtype).eps / 2
+    with torch.no_grad():
+        h = wide(x)
+        layer.load_state_dict(wide.state_dict())
+        # the inputs, the weights and three results rounded to the type, fp32's own roundings: sizes around ten
+        assert float((layer(x.to(dtype)).float() - h).abs().max()) <= (24 + 6) * (half + 2.0 ** -24) * 10
+        with torch.autocast("cuda", dtype=torch.float16):
+            assert wide(x).dtype == torch.float16
+    layer(x.to(dtype)).sum().backward()                # gamma = 0: the plain layer's gradients
+    assert layer.weight.grad.dtype == dtype and bool(layer.weight.grad.isfinite().all())
+    layer.gamma = 0.5
+    with pytest.raises(TypeError, match="float32 and bfloat16"):
+        layer(x.to(dtype))
+    with torch.autocast("cuda", dtype=torch.float16), pytest.raises(TypeError, match="float32 and bfloat16"):
+        _layer("silu", gamma=0.5)(x)
