@@ -282,6 +282,8 @@ def gated_linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Ten
     layers._act_code(act)
     layers._gated_sizes(weight)
     _check_format(index_format)
+    if not 0.0 <= gamma <= 1.0:                        # (a NaN too)
+        raise ValueError("gamma must be in [0, 1], got %r" % (gamma,))
     if torch.is_autocast_enabled("cuda") and x.is_cuda:
         dtype = torch.get_autocast_dtype("cuda")
         x, weight, bias = x.to(dtype), weight.to(dtype), bias.to(dtype) if bias is not None else None
