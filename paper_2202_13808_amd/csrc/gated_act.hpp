@@ -107,10 +107,10 @@ template <bool FAST> __device__ inline float activation_slope(float z, int act, 
     case DROPIT_ACT_RELU:
         slope = z > 0.f ? 1.f : 0.f;
         return z < 0.f ? 0.f : z;
-    default: {
-        const float s = sigmoid_of<FAST>(z);
-        slope = s * (1.f - s);
-        return s;
+    default: {                                         // s(z) s(-z): 1 - s would have nothing left from z = 17 on
+        const float e = exp_of<FAST>(-fabsf(z)), r = inverse_of<FAST>(1.f + e);
+        slope = e * r * r;
+        return z < 0.f ? e * r : r;
     }
     }
 }

@@ -1,0 +1,62 @@
+"""The activations of the gated projection far out, relative to their own size: a value or a slope that is lost there is small,
+and an allowance that does not shrink with it would not see the loss.
+
+Tolerances.  ``unit`` is a relative error: in fp32, roundings of 2^-24 of the operations and of the arguments of the exponential
+(an argument y that is rounded by 2^-24 of itself moves e^y by y 2^-24 of itself); in bf16 the hardware's exponential and
+reciprocal, 2^-20 with the same growth.  It is taken of the sum of the terms' sizes, where terms cancel.  What leaves in bf16 is
+off by half a step more, 2^-8 of itself.  Below 2^-120 fp32 runs out of bits (e^-z overflows, or the results are denormal)."""
+import math
+
+import pytest
+import torch
+
+import paper_2202_13808_amd as dropit
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+HALF = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8}
+FLOOR = 2.0 ** -120
+
+
+def gates(dtype):
+    z = torch.cat([torch.linspace(-30, 30, 1201), torch.linspace(-1, 1, 41) / 64,
+                   torch.tensor([0.0, -0.0, 40.0, -40.0, 87.0, -87.0, 90.0, -90.0, 300.0, -300.0, 1e10, -1e10, 3e18, -3e18, 1e20, -1e20, 3e38, -3e38])])
+    return z.to(DT[dtype])
+
+
+def sigmoid_bounds(z, dtype):
+    s, t = torch.sigmoid(z), torch.sigmoid(-z)
+    unit = 16 * 2.0 ** -24 if dtype == "f32" else 2.0 ** -20 * (1 + z.abs())
+    return (s, unit * s), (s * t, unit * s * t)
+
+
+BOUNDS = {"sigmoid": sigmoid_bounds}                   # (act, its tolerance), (slope, its tolerance), in 64 bits
+
+
+def near(got, want, tol, dtype, z, what):
+    diff = (got.cpu().double() - want).abs()
+    bad = ~(diff <= tol + HALF[dtype] * want.abs() + FLOOR * (1 + want.abs()))
+    assert not bool(bad.any()), (what, [(float(a), float(b), float(c)) for a, b, c in zip(z[bad][:4], got.cpu()[bad][:4], want[bad][:4])])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("act", list(BOUNDS))
+def test_activations_far_out(act, dtype):
+    print("gated tails", act, dtype, flush=True)
+    z = gates(dtype)
+    n = z.numel()
+    (value, value_tol), (slope, slope_tol) = BOUNDS[act](z.double(), dtype)
+    pre = torch.cat([z, torch.ones(n, dtype=DT[dtype])]).unsqueeze(0).to(DEV)
+    w = torch.zeros(2 * n, 8, dtype=DT[dtype], device=DEV)
+    w[:, 0] = pre[0]
+    dpre, _, _ = dropit.gated_backward(torch.ones(1, n, dtype=DT[dtype], device=DEV), pre, w, act=act, need_dx=False)
+    near(dpre[0, :n], slope, slope_tol, dtype, z, "slope")
+    near(dpre[0, n:], value, value_tol, dtype, z, "value in the gradient")
+    for tokens in (1, 70, 1500):                       # the products for few, for some and for many tokens
+        x = torch.zeros(tokens, 8, dtype=DT[dtype], device=DEV)
+        x[:, 0] = 1.0
+        h = dropit.gated_forward(x, w, act=act)
+        assert torch.equal(h, h[:1].expand_as(h))
+        near(h[0], value, value_tol, dtype, z, "value")
