@@ -101,7 +101,8 @@ template <bool FAST> __device__ inline float activation_slope(float z, int act, 
     }
     case DROPIT_ACT_GELU_TANH: {
         const float s = sigmoid_of<FAST>(2.f * TANH_K * (z + TANH_C * z * z * z));
-        slope = s + z * s * (1.f - s) * (2.f * TANH_K) * (1.f + 3.f * TANH_C * z * z);
+        const float c = fminf(fmaxf(z, -64.f), 64.f);  // (s (1 - s) is zero there; z^2 overflows from 2^64 on)
+        slope = s + c * s * (1.f - s) * (2.f * TANH_K) * (1.f + 3.f * TANH_C * c * c);
         return z * s;
     }
     case DROPIT_ACT_RELU:

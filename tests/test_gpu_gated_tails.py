@@ -32,7 +32,19 @@ def sigmoid_bounds(z, dtype):
     return (s, unit * s), (s * t, unit * s * t)
 
 
-BOUNDS = {"sigmoid": sigmoid_bounds}                   # (act, its tolerance), (slope, its tolerance), in 64 bits
+def gelu_tanh_bounds(z, dtype):
+    k, c = math.sqrt(2 / math.pi), 0.044715
+    y = 2 * k * (z + c * z ** 3)
+    s, t = torch.sigmoid(y), torch.sigmoid(-y)
+    unit = (32 + 8 * y.abs()) * 2.0 ** -24 if dtype == "f32" else 2.0 ** -20 * (1 + y.abs())
+    inner = torch.where(t > 0, 2 * k * z * (1 + 3 * c * z * z), torch.zeros_like(z))
+    # t = 1 - s is off by a rounding of 1, and is zero where it is smaller than that
+    lost = torch.where(t < 2.0 ** -25, t, torch.full_like(z, 2.0 ** -23 if dtype == "f32" else 2.0 ** -20))
+    s_off = unit * s * t + (8 * 2.0 ** -24 if dtype == "f32" else 2.0 ** -20) * s        # (the argument moves s by s t)
+    return (z * s, z.abs() * s_off), (s + s * t * inner, s_off + (unit * s * t + lost * s) * inner.abs())
+
+
+BOUNDS = {"sigmoid": sigmoid_bounds, "gelu_tanh": gelu_tanh_bounds}                   # (act, its tolerance), (slope, its tolerance), in 64 bits
 
 
 def near(got, want, tol, dtype, z, what):
