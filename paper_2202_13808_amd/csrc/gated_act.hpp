@@ -16,52 +16,39 @@ template <bool FAST> __device__ inline float inverse_of(float x) { return FAST ?
 
 template <bool FAST> __device__ inline float sigmoid_of(float z) { return inverse_of<FAST>(1.f + exp_of<FAST>(-z)); }
 
-// Phi(-|z|) = 2^P(|z|), P of degree 7 fitted to log2 of it over [0, 5.5] (largest relative error of the result, weighted with
-// |z| Phi beyond 4, made smallest): off by 3.4e-6 of itself up to |z| = 4 and never by more than 3.3e-7 / |z|; P falls for
-// ever beyond.  Seven multiply-adds and an exponential, no reciprocal: ViT-B's forward pass leaves with a third less of it.
-__device__ inline float normal_tail(float a)            // a = |z|
+// Phi(-a) = 2^P(a), P of degree 9 fitted to log2 of it over [0, 12.9], where fp32 ends: off by 8e-6 of itself up to a = 4, 2.2e-5
+// up to 8 and 8.2e-5 at the end; P falls for ever beyond.  (Degree 7 fitted to the size of a Phi(-a) was off by 3.4e-6 up to 4,
+// but by 3.6e-3 at 6 and a tenth at 8; its two multiply-adds less are 1.4 us of ViT-B's forward pass, 125.9 and 127.4 us, and as
+// much of the backward pass.)  Nine multiply-adds and an exponential, no reciprocal.
+__device__ inline float normal_tail(float a)            // 0 <= a <= 100
 {
-    float p = fmaf(a, -9.67966821e-07f, 4.85793513e-05f);
-    p = fmaf(p, a, -0.000854563057f);
-    p = fmaf(p, a, 0.00829118465f);
-    p = fmaf(p, a, -0.0536483587f);
-    p = fmaf(p, a, -0.458673029f);
-    p = fmaf(p, a, -1.1512002f);
-    return __builtin_amdgcn_exp2f(fmaf(p, a, -0.999997246f));
-}
-
-// Phi(z), and e^(-z^2 / 2) for the slope.  FAST: Abramowitz and Stegun, Handbook of Mathematical Functions, formula 7.1.26
-// for erfc(|z| / sqrt 2), halved; off by at most 1.5e-7
-template <bool FAST> __device__ inline float normal_cdf(float z, float &bell)
-{
-    bell = exp_of<FAST>(-0.5f * z * z);
-    if constexpr (!FAST) {
-        return 0.5f * erfcf(-0.70710678118654752f * z);
-    } else {
-        const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678118654752f, fabsf(z), 1.f));
-        float s = fmaf(t, 1.061405429f, -1.453152027f);
-        s = fmaf(s, t, 1.421413741f);
-        s = fmaf(s, t, -0.284496736f);
-        s = fmaf(s, t, 0.254829592f);
-        const float q = 0.5f * s * t * bell;
-        return z < 0.f ? q : 1.f - q;
-    }
+    float p = fmaf(a, -2.40522136e-09f, 1.67417483e-07f);
+    p = fmaf(p, a, -5.13553641e-06f);
+    p = fmaf(p, a, 9.20612656e-05f);
+    p = fmaf(p, a, -0.00108233339f);
+    p = fmaf(p, a, 0.00893035159f);
+    p = fmaf(p, a, -0.0545950532f);
+    p = fmaf(p, a, -0.458002746f);
+    p = fmaf(p, a, -1.15137577f);
+    return __builtin_amdgcn_exp2f(fmaf(p, a, -0.999989986f));
 }
 
 constexpr float TANH_K = 0.7978845608028654f, TANH_C = 0.044715f;           // sqrt(2 / pi)
+
+// max(z, 0) - |z| Phi(-|z|); an infinity or a NaN stays one
+__device__ inline float gelu_fast(float z)
+{
+    const float a = fminf(fabsf(z), 100.f);
+    return fmaf(-a, normal_tail(a), z < 0.f ? 0.f : z);
+}
 
 template <bool FAST> __device__ inline float activation(float z, int act)
 {
     switch (act) {                                     // (the same branch in every thread of a launch)
     case DROPIT_ACT_SILU: return FAST ? z * sigmoid_of<true>(z) : z / (1.f + expf(-z));
-    case DROPIT_ACT_GELU: {
-        if constexpr (FAST) {                          // max(z, 0) - |z| Phi(-|z|); an infinity or a NaN stays one
-            const float a = fminf(fabsf(z), 100.f);
-            return fmaf(-a, normal_tail(a), z < 0.f ? 0.f : z);
-        }
-        float bell;
-        return z * normal_cdf<FAST>(z, bell);
-    }
+    case DROPIT_ACT_GELU:
+        if constexpr (FAST) return gelu_fast(z);
+        else return z * (0.5f * erfcf(-0.70710678118654752f * z));
     case DROPIT_ACT_GELU_TANH: return z * sigmoid_of<FAST>(2.f * TANH_K * (z + TANH_C * z * z * z));    // (1 + tanh y) / 2 = sigmoid(2 y)
     case DROPIT_ACT_RELU: return z < 0.f ? 0.f : z;    // (a NaN stays one)
     default: return sigmoid_of<FAST>(z);
@@ -93,11 +80,17 @@ template <bool FAST> __device__ inline float activation_slope(float z, int act, 
         slope = s * (1.f + z * (1.f - s));
         return z * s;
     }
-    case DROPIT_ACT_GELU: {
-        float bell;
-        const float phi = normal_cdf<FAST>(z, bell);
-        slope = phi + z * bell * 0.3989422804014327f;  // 1 / sqrt(2 pi)
-        return z * phi;
+    case DROPIT_ACT_GELU: {                            // Phi(z) + z e^(-z^2 / 2) / sqrt(2 pi); the forward pass's Phi.  (From 100 on e is 0.)
+        const float c = fminf(fmaxf(z, -100.f), 100.f), bell = exp_of<FAST>(-0.5f * z * z);
+        if constexpr (FAST) {
+            const float tail = normal_tail(fabsf(c));
+            slope = (z < 0.f ? tail : 1.f - tail) + c * bell * 0.3989422804014327f;
+            return fmaf(-fabsf(c), tail, z < 0.f ? 0.f : z);
+        } else {
+            const float phi = 0.5f * erfcf(-0.70710678118654752f * z);
+            slope = phi + c * bell * 0.3989422804014327f;
+            return z * phi;
+        }
     }
     case DROPIT_ACT_GELU_TANH: {
         const float s = sigmoid_of<FAST>(2.f * TANH_K * (z + TANH_C * z * z * z));

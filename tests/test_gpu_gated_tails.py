@@ -44,7 +44,31 @@ def gelu_tanh_bounds(z, dtype):
     return (z * s, z.abs() * s_off), (s + s * t * inner, s_off + (unit * s * t + lost * s) * inner.abs())
 
 
-BOUNDS = {"sigmoid": sigmoid_bounds, "gelu_tanh": gelu_tanh_bounds}                   # (act, its tolerance), (slope, its tolerance), in 64 bits
+def gelu_bounds(z, dtype):
+    ndtr = lambda x: 0.5 * torch.special.erfc(-x * math.sqrt(0.5))  # noqa: E731  (torch.special.ndtr is 0 from -9 on)
+    phi, bell = ndtr(z), torch.exp(-0.5 * z * z) / math.sqrt(2 * math.pi)
+    near_z = z.clamp(-100, 100)
+    # the argument of both exponentials is z^2 / 2; bf16 takes Phi(-|z|) from a polynomial that is off by 1e-4 of it at most
+    unit = (32 + 2 * near_z ** 2) * 2.0 ** -24 if dtype == "f32" else 2.0 ** -20 * (1 + near_z ** 2)
+    tail = unit if dtype == "f32" else 1e-4
+    phi_off = tail * ndtr(-z.abs()) + (4 * 2.0 ** -24) * phi
+    return (z * phi, z.abs() * phi_off), (phi + near_z * bell, phi_off + unit * (near_z * bell).abs())
+
+
+def silu_bounds(z, dtype):
+    s, t = torch.sigmoid(z), torch.sigmoid(-z)
+    unit = 16 * 2.0 ** -24 if dtype == "f32" else 2.0 ** -20 * (1 + z.clamp(-100, 100).abs())
+    lost = torch.where(t < 2.0 ** -25, t, torch.full_like(z, 2.0 ** -23 if dtype == "f32" else 2.0 ** -20))       # t = 1 - s
+    return (z * s, (unit * z * s).abs()), (s * (1 + z * t), unit * s * (1 + z.abs() * t) + lost * s * z.abs())
+
+
+def relu_bounds(z, dtype):
+    nothing = torch.zeros_like(z)
+    return (z.clamp(min=0), nothing), ((z > 0).double(), nothing)
+
+
+# (act, its tolerance), (slope, its tolerance), in 64 bits
+BOUNDS = {"sigmoid": sigmoid_bounds, "gelu_tanh": gelu_tanh_bounds, "gelu": gelu_bounds, "silu": silu_bounds, "relu": relu_bounds}
 
 
 def near(got, want, tol, dtype, z, what):
