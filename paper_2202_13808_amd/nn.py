@@ -23,6 +23,7 @@ from typing import Iterator, List, Optional, Sequence, Tuple, Union
 
 import torch
 import torch.nn.functional as F
+from torch.autograd import forward_ad
 
 from . import binding, layers
 
@@ -260,7 +261,9 @@ def _followed(*tensors: Optional[torch.Tensor]) -> bool:
     function transform, a trace): it would not see the library's kernels, and its result would miss them."""
     if torch.jit.is_tracing() or (_transforms_active is not None and _transforms_active()):
         return True
-    return any(t is not None and torch.autograd.forward_ad.unpack_dual(t).tangent is not None for t in tensors)
+    if getattr(forward_ad, "_current_level", 0) < 0:   # (no dual tensors anywhere: asking the tensors takes 3 us)
+        return False
+    return any(t is not None and forward_ad.unpack_dual(t).tangent is not None for t in tensors)
 
 
 def _gated_plain(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor], act: str) -> torch.Tensor:

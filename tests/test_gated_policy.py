@@ -3,6 +3,7 @@ import math
 
 import pytest
 import torch
+import torch.autograd.forward_ad as fwad
 
 from paper_2202_13808_amd import nn as dnn
 
@@ -14,3 +15,19 @@ def test_gated_linear_refuses_rates_that_are_none(gamma):
         with pytest.raises(ValueError, match="gamma"):
             dnn.gated_linear(x, weight, gamma=gamma)
     assert dnn.gated_linear(x, w, gamma=0.0).shape == (2, 3) and dnn.gated_linear(x, w, gamma=1.0).shape == (2, 3)
+
+
+def test_dual_tensors_transforms_and_traces_are_noticed():
+    x = torch.ones(3)
+    assert not dnn._followed(x, None, x)
+    with fwad.dual_level():
+        dual = fwad.make_dual(x, x)
+        assert dnn._followed(x, dual) and dnn._followed(dual, None) and not dnn._followed(x, None)
+        with torch.no_grad():
+            assert dnn._followed(dual)
+    assert not dnn._followed(x)
+    seen = []
+    torch.func.jvp(lambda t: seen.append(dnn._followed(t)) or t, (x,), (x,))
+    torch.func.vmap(lambda t: seen.append(dnn._followed(t)) or t)(x)
+    torch.jit.trace(lambda t: seen.append(dnn._followed(t)) or t + 1, (x,), check_trace=False)
+    assert seen == [True, True, True] and not dnn._followed(x)
