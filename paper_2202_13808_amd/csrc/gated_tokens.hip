@@ -125,10 +125,13 @@ bool gated_tokens_takes(int64_t tokens, int64_t c_in, int64_t hidden, dropit_dty
     const int64_t size = dt == DROPIT_BF16 ? 2 : 4;
     if (c_in % (16 / size) != 0) return false;         // rows in 16-byte units
     if (hidden > 1 << 26) return false;                // a launch has fewer than 2^32 threads
-    // Every workgroup reads all tokens.  Up to 16 that is always worth it; up to 64 while the weights are small (us for 64 tokens
-    // here and in gated.hip's product: bf16 768 -> 2048 7.3 and 12.4, 2048 -> 5632 (46 MB) 25.7 and 24.9, 4096 -> 10240 80.6
-    // and 55.7; fp32 768 -> 2048 15.3 and 20.7, 2048 -> 5632 83 and 48)
-    return tokens <= 16 || (tokens <= 64 && 2 * hidden * c_in * size <= int64_t(32) << 20);
+    // Every workgroup reads all tokens.  Up to 16 that is always worth it, beyond while the weights are small (us, calls in a row
+    // in a graph, here and in the product that takes the call otherwise).  bf16, 32 tokens: 256 -> 704 3.4 and 4.8, 768 -> 2048 5.2 and 6.1,
+    // 2048 -> 4096 12.3 and 13.1; 64 tokens: 4.6 and 7.6, 7.2 and 12.2, 16.9 and 17.8; with more than 32 MB of weights, 2048 ->
+    // 5632 at 32 tokens 18.6 and 14.3, at 64 26.4 and 18.5, 4096 -> 10240 58 and 45.5, 80 and 42.6.  fp32, 32 tokens: 256 -> 704
+    // 5.4 and 7.6, 768 -> 2048 10.8 and 9.9, 1024 -> 2688 12.9 and 16.2; 64 tokens: 7.7 and 8.3, 15.8 and 10.5, 21.4 and 17.8,
+    // so that its limit is 32.
+    return tokens <= 16 || (tokens <= (dt == DROPIT_BF16 ? 64 : 32) && 2 * hidden * c_in * size <= int64_t(32) << 20);
 }
 
 dropit_status launch_gated_tokens(const void *x, int64_t tokens, int c_in, dropit_dtype dt, const void *w, const void *bias,
@@ -148,8 +151,7 @@ dropit_status launch_gated_tokens(const void *x, int64_t tokens, int c_in, dropi
     } else {
         if (tokens <= 8) launch(gated_tokens_kernel<false, 2, 1>);
         else if (tokens <= 16) launch(gated_tokens_kernel<false, 1, 1>);
-        else if (tokens <= 32) launch(gated_tokens_kernel<false, 1, 2>);
-        else launch(gated_tokens_kernel<false, 1, 4>);
+        else launch(gated_tokens_kernel<false, 1, 2>);
     }
     return launch_status();
 }
