@@ -441,9 +441,11 @@ dropit_status launch(const WideArgs &a, hipStream_t stream)
 
 WidePlan gated_wide_plan(int64_t tokens, int64_t c_in, int64_t hidden, bool forward)
 {
-    // the weights, and 256 tokens, below 2^31 bytes.  Few tokens leave most of a tile empty, but its
-    // slices fill the chip (us for the gradients of 16 tokens, here and in gated.hip's product: 384 -> 1024 15 and 19, 2048 ->
-    // 5632 23 and 46, 4096 -> 10240 45 and 115)
+    // the weights, and 256 tokens, below 2^31 bytes.  Few tokens leave most of a tile empty, but in the gradients its slices fill
+    // the chip (us for 16 tokens, here and in gated.hip's product: 384 -> 1024 15 and 19, 2048 -> 5632 23 and 46, 4096 -> 10240 45
+    // and 115).  The forward pass's pay from 33 tokens on (32 tokens: 2048 -> 5632 16.4 and 14.3, 4096 -> 7168 30.0 and 32.0, 8192
+    // -> 4096 35.1 and 36.1, 4096 -> 10240 38.9 and 45.5, the largest difference; 17 tokens: 16.0 and 14.1, 29.2 and 28.8, 35.8 and
+    // 34.3, 38.3 and 42.8)
     WidePlan plan{(!forward || tokens > 32) && 4 * hidden * c_in < int64_t(1) << 31 && std::max(c_in, 2 * hidden) < (1 << 22) - 8, 2, 1, 0.0};
     if (!plan.takes) return plan;
     // How many tokens to a tile, and how many slices of the sum: what the compute unit with the most tiles takes, a block of
