@@ -27,9 +27,9 @@ extern "C" {
  * h is computed from the unrounded fp32 pre and rounded once; pre, where it is asked for, is rounded once too.
  *     DROPIT_ACT_SILU z / (1 + e^-z), DROPIT_ACT_GELU z * Phi(z), DROPIT_ACT_GELU_TANH its tanh form
  *     z / 2 * (1 + tanh(sqrt(2 / pi) * (z + 0.044715 z^3))), DROPIT_ACT_RELU max(z, 0), DROPIT_ACT_SIGMOID 1 / (1 + e^-z)
- * bf16 evaluates them with the hardware's exponential and reciprocal (a relative 2^-20 or so, times the exponent; Phi, in the
- * slope too, by a fitted polynomial whose smaller tail Phi(-|z|) is off by 8e-6 of itself up to |z| = 4, 2.2e-5 up to 8 and 1e-4
- * up to 12.9, where it leaves fp32's range), fp32 with the fp32 math library.
+ * bf16 evaluates them with the hardware's exponential and reciprocal (a relative 2^-20 or so, times the exponent; the forward
+ * pass's Phi(z) by a fitted polynomial whose smaller tail Phi(-|z|) is off by 8e-6 of itself up to |z| = 4, 2.2e-5 up to 8 and
+ * 1e-4 up to 12.9, where it leaves fp32's range), fp32 with the fp32 math library.
  *
  * x [tokens, c_in], w, bias, h, pre: device, row-major, type dt, 16-byte aligned; pre may be NULL (inference).
  * 0 <= tokens < 2^31, 1 <= c_in <= 2^28, 1 <= hidden <= 2^27, and ceil(tokens / 64) times the larger of ceil(hidden / 32) and

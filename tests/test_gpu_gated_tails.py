@@ -26,13 +26,13 @@ def gates(dtype):
     return z.to(DT[dtype])
 
 
-def sigmoid_bounds(z, dtype):
+def sigmoid_bounds(z, dtype, forward):
     s, t = torch.sigmoid(z), torch.sigmoid(-z)
     unit = 16 * 2.0 ** -24 if dtype == "f32" else 2.0 ** -20 * (1 + z.abs())
     return (s, unit * s), (s * t, unit * s * t)
 
 
-def gelu_tanh_bounds(z, dtype):
+def gelu_tanh_bounds(z, dtype, forward):
     k, c = math.sqrt(2 / math.pi), 0.044715
     y = 2 * k * (z + c * z ** 3)
     s, t = torch.sigmoid(y), torch.sigmoid(-y)
@@ -44,25 +44,26 @@ def gelu_tanh_bounds(z, dtype):
     return (z * s, z.abs() * s_off), (s + s * t * inner, s_off + (unit * s * t + lost * s) * inner.abs())
 
 
-def gelu_bounds(z, dtype):
+def gelu_bounds(z, dtype, forward):
     ndtr = lambda x: 0.5 * torch.special.erfc(-x * math.sqrt(0.5))  # noqa: E731  (torch.special.ndtr is 0 from -9 on)
     phi, bell = ndtr(z), torch.exp(-0.5 * z * z) / math.sqrt(2 * math.pi)
     near_z = z.clamp(-100, 100)
-    # the argument of both exponentials is z^2 / 2; bf16 takes Phi(-|z|) from a polynomial that is off by 1e-4 of it at most
+    # the argument of both exponentials is z^2 / 2; bf16's forward pass takes Phi(-|z|) from a polynomial that is off by 1e-4 of it
+    # at most
     unit = (32 + 2 * near_z ** 2) * 2.0 ** -24 if dtype == "f32" else 2.0 ** -20 * (1 + near_z ** 2)
-    tail = unit if dtype == "f32" else 1e-4
+    tail = 1e-4 if dtype == "bf16" and forward else unit
     phi_off = tail * ndtr(-z.abs()) + (4 * 2.0 ** -24) * phi
     return (z * phi, z.abs() * phi_off), (phi + near_z * bell, phi_off + unit * (near_z * bell).abs())
 
 
-def silu_bounds(z, dtype):
+def silu_bounds(z, dtype, forward):
     s, t = torch.sigmoid(z), torch.sigmoid(-z)
     unit = 16 * 2.0 ** -24 if dtype == "f32" else 2.0 ** -20 * (1 + z.clamp(-100, 100).abs())
     lost = torch.where(t < 2.0 ** -25, t, torch.full_like(z, 2.0 ** -23 if dtype == "f32" else 2.0 ** -20))       # t = 1 - s
     return (z * s, (unit * z * s).abs()), (s * (1 + z * t), unit * s * (1 + z.abs() * t) + lost * s * z.abs())
 
 
-def relu_bounds(z, dtype):
+def relu_bounds(z, dtype, forward):
     nothing = torch.zeros_like(z)
     return (z.clamp(min=0), nothing), ((z > 0).double(), nothing)
 
@@ -83,13 +84,17 @@ def test_activations_far_out(act, dtype):
     print("gated tails", act, dtype, flush=True)
     z = gates(dtype)
     n = z.numel()
-    (value, value_tol), (slope, slope_tol) = BOUNDS[act](z.double(), dtype)
+    (value, value_tol), (slope, slope_tol) = BOUNDS[act](z.double(), dtype, False)
     pre = torch.cat([z, torch.ones(n, dtype=DT[dtype])]).unsqueeze(0).to(DEV)
     w = torch.zeros(2 * n, 8, dtype=DT[dtype], device=DEV)
     w[:, 0] = pre[0]
-    dpre, _, _ = dropit.gated_backward(torch.ones(1, n, dtype=DT[dtype], device=DEV), pre, w, act=act, need_dx=False)
+    dpre, _, dbias = dropit.gated_backward(torch.ones(1, n, dtype=DT[dtype], device=DEV), pre, w, act=act, need_dx=False, need_dbias=True)
+    # (one token: the sums of its gradients are those gradients, not rounded)
+    near(dbias[:n], slope, slope_tol, "f32", z, "slope in the sum")
+    near(dbias[n:], value, value_tol, "f32", z, "value in the sum")
     near(dpre[0, :n], slope, slope_tol, dtype, z, "slope")
     near(dpre[0, n:], value, value_tol, dtype, z, "value in the gradient")
+    value_tol = BOUNDS[act](z.double(), dtype, True)[0][1]
     for tokens in (1, 70, 1500):                       # the products for few, for some and for many tokens
         x = torch.zeros(tokens, 8, dtype=DT[dtype], device=DEV)
         x[:, 0] = 1.0
