@@ -11,7 +11,7 @@
 // The arithmetic is that of single fp32 operations, correctly rounded division and square root included: the codes and the
 // residual's 16 bits are exact functions of the inputs, which any other implementation of the formulas reproduces.
 //
-// Measured: 21.8 M fp32 parameters in 152 tensors 134 us, 4.5 TB/s of the 5.1 that a large copy reaches; 269 M bf16 parameters in
+// Measured: 21.8 M fp32 parameters in 150 tensors 134 us, 4.5 TB/s of the 5.1 that a large copy reaches; 269 M bf16 parameters in
 // 16 tensors with 8-bit states 620 us, 4.3 TB/s.
 #include <cmath>
 #include <type_traits>
@@ -34,7 +34,7 @@ constexpr uint32_t MAX_CHUNKS = 1u << 23;
 static_assert(ADAMW_MAX_NUMEL / ADAMW_CHUNK <= MAX_CHUNKS && ADAMW_MAX_NUMEL / (ADAMW_THREADS * ADAMW_PER_THREAD) <= MAX_CHUNKS, "");
 
 // p, g, m, v, then the offsets of 8-bit states, then the residual: what a kind of step needs of each tensor.  As many tensors as
-// keep the arguments under 4 KB (48 of them took 4 launches for the 152 tensors of a 12-block encoder, 147 us for 140)
+// keep the arguments under 4 KB (48 of them took 4 launches for the 150 tensors of a 12-block encoder, 147 us for 140)
 template <bool RESIDUAL, bool BITS8> struct AdamwTable {
     static constexpr int POINTERS = 4 + (BITS8 ? 2 : 0) + (RESIDUAL ? 1 : 0);
     static constexpr int MOST = (4096 - 128) / (POINTERS * 8 + 12);

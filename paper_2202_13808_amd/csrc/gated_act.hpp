@@ -16,10 +16,10 @@ template <bool FAST> __device__ inline float inverse_of(float x) { return FAST ?
 
 template <bool FAST> __device__ inline float sigmoid_of(float z) { return inverse_of<FAST>(1.f + exp_of<FAST>(-z)); }
 
-// The forward pass's Phi, for a bf16 result: Phi(-a) = 2^P(a), P of degree 9 fitted to log2 of it over [0, 12.9], where fp32 ends: off by 8e-6 of itself up to a = 4, 2.2e-5
-// up to 8 and 8.2e-5 at the end; P falls for ever beyond.  (Degree 7 fitted to the size of a Phi(-a) was off by 3.4e-6 up to 4,
-// but by 3.6e-3 at 6 and a tenth at 8; its two multiply-adds less are 1.4 us of ViT-B's forward pass, 125.9 and 127.4 us.)
-// Nine multiply-adds and an exponential, no reciprocal.
+// The forward pass's Phi, for a bf16 result: Phi(-a) = 2^P(a), P of degree 9 fitted to log2 of it over [0, 12.9], where fp32
+// ends: off by 8e-6 of itself up to a = 4, 2.2e-5 up to 8 and 8.2e-5 at the end; P falls for ever beyond.  (Degree 7 fitted to
+// the size of a Phi(-a) was off by 3.4e-6 up to 4, but by 3.6e-3 at 6 and a tenth at 8; its two multiply-adds less are 1.4 us of
+// ViT-B's forward pass, 125.9 and 127.4 us.)  Nine multiply-adds and an exponential, no reciprocal.
 __device__ inline float normal_tail(float a)            // 0 <= a <= 100
 {
     float p = fmaf(a, -2.40522136e-09f, 1.67417483e-07f);
@@ -35,8 +35,8 @@ __device__ inline float normal_tail(float a)            // 0 <= a <= 100
 
 // The slopes' Phi, whose sums over the tokens leave in fp32: Phi(-a) = e^(-a^2 / 2) t Q(t), t = 1 / (1 + 0.305 a), Q of degree 7
 // fitted to the ratio over [0, 13.3], largest relative error made smallest: 6e-8, in fp32 5e-7 with the reciprocal's, and the
-// exponential's on top, which the slope needs anyhow.  (ViT-B's
-// backward pass takes 137.0 us with it, 136.9 with formula 7.1.26 of Abramowitz and Stegun, 1 % off at 8.)
+// exponential's on top, which the slope needs anyhow.  (ViT-B's backward pass takes 137.3 us with it, 136.9 with formula 7.1.26 of
+// Abramowitz and Stegun, which is 1 % off at 8.)
 __device__ inline float normal_tail_of(float a, float bell)                 // bell = e^(-a^2 / 2)
 {
     const float t = __builtin_amdgcn_rcpf(fmaf(0.304987103f, a, 1.f));

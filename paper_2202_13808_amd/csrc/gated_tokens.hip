@@ -1,9 +1,9 @@
 // The gated projection's forward pass for few tokens (decoding): one pass over the weights.
 //
-// Bound by reading the weights: 16 tokens 4096 -> 10240 in bf16 35 us, 4.8 TB/s of them.  A workgroup of eight wavefronts takes 16 hidden columns, 16 gate rows and the 16 up rows of
-// the same columns, each wavefront an eighth of the sum, so that even a small layer has enough loads in flight.  Both operands
-// go from memory straight into the registers of the 16 x 16 matrix instructions, with no LDS between; the eighths meet in LDS,
-// in ascending order.
+// Bound by reading the weights: 16 tokens 4096 -> 10240 in bf16 35 us, 4.8 TB/s of them.  A workgroup of eight wavefronts takes
+// 16 hidden columns, 16 gate rows and the 16 up rows of the same columns, each wavefront an eighth of the sum, so that even a
+// small layer has enough loads in flight.  Both operands go from memory straight into the registers of the 16 x 16 matrix
+// instructions, with no LDS between; the eighths meet in LDS, in ascending order.
 //
 // Lane l of an operand holds slot l % 16, so sixteen neighbouring lanes that were sixteen rows would touch sixteen cache
 // lines a quarter of a load.  Instead the slots are 16 / P rows in P parts each: neighbouring lanes hold neighbouring 16 bytes
@@ -126,11 +126,11 @@ bool gated_tokens_takes(int64_t tokens, int64_t c_in, int64_t hidden, dropit_dty
     if (c_in % (16 / size) != 0) return false;         // rows in 16-byte units
     if (hidden > 1 << 26) return false;                // a launch has fewer than 2^32 threads
     // Every workgroup reads all tokens.  Up to 16 that is always worth it, beyond while the weights are small (us, calls in a row
-    // in a graph, here and in the product that takes the call otherwise).  bf16, 32 tokens: 256 -> 704 3.4 and 4.8, 768 -> 2048 5.2 and 6.1,
-    // 2048 -> 4096 12.3 and 13.1; 64 tokens: 4.6 and 7.6, 7.2 and 12.2, 16.9 and 17.8; with more than 32 MB of weights, 2048 ->
-    // 5632 at 32 tokens 18.6 and 14.3, at 64 26.4 and 18.5, 4096 -> 10240 58 and 45.5, 80 and 42.6.  fp32, 32 tokens: 256 -> 704
-    // 5.4 and 7.6, 768 -> 2048 10.8 and 9.9, 1024 -> 2688 12.9 and 16.2; 64 tokens: 7.7 and 8.3, 15.8 and 10.5, 21.4 and 17.8,
-    // so that its limit is 32.
+    // in a graph, here and in the product that takes the call otherwise).  bf16, 32 tokens: 256 -> 704 3.4 and 4.8, 768 -> 2048
+    // 5.2 and 6.1, 2048 -> 4096 12.3 and 13.1; 64 tokens: 4.6 and 7.6, 7.2 and 12.2, 16.9 and 17.8; with more than 32 MB of
+    // weights, 2048 -> 5632 at 32 tokens 18.6 and 14.3, at 64 26.4 and 18.5, 4096 -> 10240 58 and 45.5, 80 and 42.6.  fp32, 32
+    // tokens: 256 -> 704 5.4 and 7.6, 768 -> 2048 10.8 and 9.9, 1024 -> 2688 12.9 and 16.2; 64 tokens: 7.7 and 8.3, 15.8 and
+    // 10.5, 21.4 and 17.8, so that its limit is 32.
     return tokens <= 16 || (tokens <= (dt == DROPIT_BF16 ? 64 : 32) && 2 * hidden * c_in * size <= int64_t(32) << 20);
 }
 

@@ -450,7 +450,8 @@ WidePlan gated_wide_plan(int64_t tokens, int64_t c_in, int64_t hidden, bool forw
     if (!plan.takes) return plan;
     // How many tokens to a tile, and how many slices of the sum: what the compute unit with the most tiles takes, a block of
     // the sum and a tile's start and end at what they were measured to cost (us; whole chip busy: blocks of 8192 tokens 4096 ->
-    // 10240 both ways, ends of ViT-B's and DeiT-S's forward passes).  Fewer tokens cost more LDS reads per matrix instruction:
+    // 10240 both ways, ends of ViT-B's and DeiT-S's forward passes, which keep the pre-activations: without them an end stores a
+    // third, and the gradients' half or less, so that there a wide end is counted for more than it takes).  Fewer tokens cost more LDS reads per matrix instruction:
     // 64 of them as much as 128 per block, so there is no such tile.  us for 256, 192 and 128 tokens: 12608 tokens 768 -> 2048
     // forward 109, 105, 123, backward 81, 74, 108; 25216 tokens 384 -> 1024 75, 73, 77 and 50, 67, 59; 2048 tokens 2048 ->
     // 5632 93, 84, 93 and 169, 137, 128; 8192 tokens 4096 -> 10240 1004, 1095, 1365.  Slices cost a launch and their partial

@@ -1,5 +1,5 @@
 // What a call over hundreds of tensors has to know of each of them, in one pass: address, number of elements, type, device,
-// whether it is contiguous.  Asked for from Python, each of these costs 70 ns a tensor; twenty of them for a step over 152
+// whether it is contiguous.  Asked for from Python, each of these costs 70 ns a tensor; twenty of them for a step over 150
 // tensors took 150 us of host time, longer than the step's kernels.  Only reads the tensors; the kernels stay behind the C ABI.
 #include <Python.h>
 
