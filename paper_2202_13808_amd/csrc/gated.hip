@@ -477,7 +477,7 @@ dropit_status launch_wide(GenArgs a, const WideLayout &l, void *workspace, hipSt
 // ---------------------------------------------------------------------------
 // dpre from dh and pre, and the partial column sums for dbias.  A thread takes 8 (bf16) or 4 (fp32) gate columns, the up
 // columns beside them and every fourth row of a block of rows; the four row groups' sums meet in LDS.  Bound by the bytes of dh,
-// pre and dpre: 12608 tokens of 2048 columns in bf16 (258 MB) 52 us, 4.9 TB/s, a copy's rate.
+// pre and dpre: 12608 tokens of 2048 columns in bf16 (258 MB) 54.6 us, 4.7 TB/s, where a copy reaches 5.1.
 //
 // In bf16 the input gradient is a product of dpre as it is rounded here, the dpre that the caller gets and that the weight
 // gradient reads: all of them are gradients of one dpre, of the type that the matrix instructions take.  dx is 2.35e-3 off so,

@@ -1,6 +1,6 @@
 // The gated projection's products on wide tiles: bf16, many tokens (gated.hip takes every other size and type).  Bound by the matrix
-// instructions and, in large products, by the clock that the chip's power leaves them: 8192 tokens 4096 -> 10240 1000 us, 1375
-// TFLOP/s, where a plain library product of these sizes takes 947 without activation and product.
+// instructions and, in large products, by the clock that the chip's power leaves them: 8192 tokens 4096 -> 10240 990 to 1045 us by
+// the card, 1315 to 1390 TFLOP/s, where a plain library product of these sizes takes 947 without activation and product.
 //
 // A workgroup of eight wavefronts computes 256 rows of the weight operand by 64 * FN tokens, the sum in blocks of 64: 128
 // bytes of a row, a whole cache line.  (A load of 16 half lines takes the cache twice as long as one of 8 whole ones; blocks

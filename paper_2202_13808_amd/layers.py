@@ -203,7 +203,7 @@ def adamw(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], m: Sequ
           m_offset: Optional[Sequence[torch.Tensor]] = None, v_offset: Optional[Sequence[torch.Tensor]] = None,
           residual: Optional[Sequence[torch.Tensor]] = None, grad_scale: Optional[torch.Tensor] = None,
           stream=None) -> None:
-    """dropit_adamw: one AdamW step over the tensors of the lists, in place.  ``m`` / ``v`` are fp32, or uint8 codes
+    """dropit_adamw: one AdamW step over the tensors of the lists, on one device, in place.  ``m`` / ``v`` are fp32, or uint8 codes
     with int16 ``m_offset`` / ``v_offset`` of ceil(numel / 256) entries each (8-bit states).  ``residual`` (int16, as
     many elements as the parameter) makes bf16 parameters exact fp32 masters.  ``step`` counts from 1; as an int32
     device tensor it is read when the kernels run, which a captured graph needs.  ``grad_scale`` is a device scalar
@@ -288,7 +288,7 @@ def adamw_unpack(codes: torch.Tensor, offset: torch.Tensor, signed: bool, values
 def grad_norm(grads: Sequence[torch.Tensor], max_norm: float = math.inf, out: Optional[torch.Tensor] = None,
               workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """dropit_grad_norm: float32 [2] on the device, the 2-norm over all elements of ``grads`` (float32 or bfloat16, mixed
-    as they come) and min(1, max_norm / (norm + 1e-6)), the factor that clips them."""
+    as they come, on one device) and min(1, max_norm / (norm + 1e-6)), the factor that clips them."""
     count = len(grads)
     if not float(max_norm) > 0.0:
         raise ValueError("max_norm must be positive, got %r" % (max_norm,))
