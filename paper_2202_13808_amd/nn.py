@@ -279,9 +279,9 @@ def gated_linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Ten
     both projections, the activation (silu, gelu, gelu_tanh, relu, sigmoid) and the product in one kernel.  The backward pass
     takes the weight gradient from the min-k cache of ``x`` (``gamma`` = 0 keeps ``x`` itself; ``seed`` and ``index_format``
     as for ``linear``) and keeps the pre-activations whole.  Under autocast the operands are cast as ``F.linear``'s are.
-    Where nothing requires a gradient, forward-mode differentiation, ``torch.func`` and ``torch.jit.trace`` get the formula in
-    torch's operators, which they can follow; through the dropping layer they are refused.  Types other than float32 and bfloat16
-    run in torch's operators too where nothing is dropped, and are refused where something is."""
+    Where nothing is dropped, forward-mode differentiation, ``torch.func`` and ``torch.jit.trace`` get the formula in torch's
+    operators, which they can follow, and types other than float32 and bfloat16 run so too; where something is, these types,
+    forward mode and ``torch.func`` are refused."""
     layers._act_code(act)
     layers._gated_sizes(weight)
     _check_format(index_format)
@@ -290,16 +290,15 @@ def gated_linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Ten
     if torch.is_autocast_enabled("cuda") and x.is_cuda:
         dtype = torch.get_autocast_dtype("cuda")
         x, weight, bias = x.to(dtype), weight.to(dtype), bias.to(dtype) if bias is not None else None
+    dropping = gamma > 0.0 and torch.is_grad_enabled() and weight.requires_grad
+    if dropping and not x.is_cuda:
+        raise RuntimeError("DropIT layers train on device tensors only: there is no CPU path")
     if not x.is_cuda:
-        if gamma > 0.0 and torch.is_grad_enabled() and weight.requires_grad:
-            raise RuntimeError("DropIT layers train on device tensors only: there is no CPU path")
         return _gated_plain(x, weight, bias, act)
     with torch.autocast("cuda", enabled=False):
-        if x.dtype not in _KERNEL_DTYPES and not (gamma > 0.0 and torch.is_grad_enabled() and weight.requires_grad):
+        if not dropping and (x.dtype not in _KERNEL_DTYPES or _followed(x, weight, bias)):
             return _gated_plain(x, weight, bias, act)
         if not torch.is_grad_enabled() or not any(t is not None and t.requires_grad for t in (x, weight, bias)):
-            if _followed(x, weight, bias):
-                return _gated_plain(x, weight, bias, act)
             return layers.gated_forward(_contiguous(x), _contiguous(weight), _contiguous(bias) if bias is not None else None, act=act)
         if x.numel() == 0:
             gamma = 0.0

@@ -100,3 +100,21 @@ def test_types_without_a_kernel_run_plainly_where_nothing_is_dropped(dtype):
         layer(x.to(dtype))
     with torch.autocast("cuda", dtype=torch.float16), pytest.raises(TypeError, match="float32 and bfloat16"):
         _layer("silu", gamma=0.5)(x)
+
+
+def test_a_layer_that_trains_without_dropping_is_followed_too():
+    print("gated forward mode, nothing dropped", flush=True)
+    layer = _layer("silu", gamma=0.0)
+    x, v = torch.randn(3, 24, device=DEV), torch.randn(3, 24, device=DEV)
+    want = _tangent(layer, x, v, "silu")
+    with fwad.dual_level():
+        out = fwad.unpack_dual(layer(fwad.make_dual(x, v)))
+        assert float((out.tangent.detach().cpu().double() - want).abs().max()) <= 64 * 2.0 ** -24 * 10
+    grad = torch.func.grad(lambda t: layer(t).sum())(x)
+    xr = x.clone().requires_grad_(True)
+    layer(xr).sum().backward()                         # the kernels'
+    assert float((grad - xr.grad).abs().max()) <= 64 * 2.0 ** -24 * 10
+    frozen = _layer("silu", gamma=0.5).requires_grad_(False)
+    with fwad.dual_level():
+        out = fwad.unpack_dual(frozen(fwad.make_dual(xr, v)))
+        assert float((out.tangent.detach().cpu().double() - want).abs().max()) <= 64 * 2.0 ** -24 * 10
